@@ -303,7 +303,8 @@ def _handles(st):
         _scorer = ps.Scorer(0)
     case, w = st["case"], st["window"]
     st["kv"] = ps.KvCache(**st["cache"])
-    st["win"] = ps.KvWindow(w["pages"], w["reqs"], w["ctx"], w["q_off"], w["n_req"], w["n_rows"])
+    st["win"] = ps.KvWindow(w["pages"], w["reqs"], w["ctx"], w["q_off"], w["n_req"], w["n_rows"],
+                            n_pages=w["n_pages"])
     if "q" in st:
         st["plan"] = _scorer.attend_plan(case["heads"], case["kv_heads"], case["dim"], case["block"],
                                          max_req=w["n_req"], max_rows=w["n_rows"])
