@@ -443,6 +443,149 @@ ps_status ps_feedback_output(ps_ctx* ctx, const int32_t* out_len, int32_t n);
 /* Current EMA factors (n_seg entries) and L_out; either pointer may be NULL. */
 ps_status ps_read_model(ps_ctx* ctx, float* gamma, float* lout, int32_t* n_seg);
 
+/*
+ * The block cache: what the chains of a window name, on the instance that
+ * serves it.  The scheduler knows a cached block by its hash; an instance
+ * keeps its keys and values in a page.  The calls below take the scheduler's
+ * request descriptors (a shared prefix segment and a tail, ps_req) over a pool
+ * of page numbers instead of hashes: they write the new tokens' rows into the
+ * pages, read rows back, and compute the attention of the new rows over their
+ * request's chain.  They need a context but no snapshot.  Every pointer in the
+ * structs is a device pointer of the context's device, owned by the caller;
+ * the structs themselves are host memory, read before the call returns.
+ */
+#define PS_T_BF16 0
+#define PS_T_F16 1
+#define PS_T_E4M3 2 /* 8 bits (OCP e4m3), with one power of two per token and head */
+#define PS_MAX_HEADS 1024      /* query heads */
+#define PS_MAX_KV_HEADS 128    /* key / value heads */
+#define PS_MAX_HEAD_DIM 256
+#define PS_MAX_WINDOW_REQ 8192 /* requests of an attention plan */
+#define PS_MAX_ROWS 1048576    /* rows of a window in the calls below */
+
+/*
+ * Pages of one layer.  Page p holds block_tokens tokens of n_kv_heads heads:
+ * element e of slot s of head h is k[p * page_stride + (h * block_tokens + s) *
+ * head_dim + e], v alike; page_stride (elements) is at least n_kv_heads *
+ * block_tokens * head_dim, more where a page holds something else too.
+ * PS_T_E4M3: the value is that element times 2^(x - 127) with
+ * x = k_exp[p * exp_page_stride + h * block_tokens + s] in [1, 254] (the
+ * exponent arrays are NULL for the 16-bit types).  head_dim is a multiple of
+ * 16 up to PS_MAX_HEAD_DIM, block_tokens in [1, PS_MAX_BLOCK_TOKENS]; k, v and
+ * the pages' starts are 16-byte aligned.
+ */
+typedef struct {
+  void* k;
+  void* v;
+  uint8_t* k_exp;
+  uint8_t* v_exp;
+  int64_t n_pages, page_stride, exp_page_stride;
+  int32_t n_kv_heads, head_dim, block_tokens, dtype;
+} ps_kv_cache;
+
+/*
+ * A window of requests.  Request r's chain is pages[pre_off..+pre_len) ++
+ * pages[tail_off..+tail_len) of reqs[r]: token t lies in page chain[t /
+ * block_tokens], slot t % block_tokens.  ctx_tok[r] tokens of it exist (the
+ * last block may be part full); the rows row_off[r]..row_off[r + 1] (row_off
+ * has n_req + 1 entries, ascending, within [0, n_rows]) are the last ones of
+ * them, in order: row j of m is the token at position ctx_tok[r] - m + j.  A
+ * row whose position is negative has no token.  Rows outside
+ * [row_off[0], row_off[n_req]) belong to no request and are left as they are
+ * (a padded batch).  Page numbers are in [0, n_pages).
+ */
+typedef struct {
+  const int32_t* pages;
+  const ps_req* reqs;
+  const int32_t* ctx_tok;
+  const int32_t* row_off;
+  int64_t pages_len, n_pages;
+  int32_t n_req, n_rows;
+} ps_kv_window;
+
+/* Rows of heads: element e of head h of row i is data[i * row_stride +
+ * h * head_stride + e] (strides in elements, multiples of 8; data 16-byte
+ * aligned; PS_T_BF16 or PS_T_F16). */
+typedef struct {
+  void* data;
+  int64_t row_stride, head_stride;
+  int32_t dtype;
+} ps_rows;
+
+/*
+ * Write the window's rows of keys and values into their pages.  16-bit caches
+ * take rows of their own type as they are.  PS_T_E4M3 quantises each row and
+ * head: with m its largest finite magnitude, x - 127 is the least exponent e
+ * in [-126, 127] with m <= 448 * 2^e, and an element is rounded once, to the
+ * nearest even multiple, as element * 2^-e; infinities become +-448, NaN stays
+ * NaN.  Rows without a token, of a malformed request (see
+ * ps_attend_plan_dev) or in a page outside [0, window.n_pages) are not written;
+ * nor are other slots of the pages.  Rows that name the same slot (one page
+ * in two chains) must hold the same values.  Asynchronous on `hip_stream`; no
+ * allocation, so it can be captured.  PS_E_INVAL / PS_E_RANGE, before any
+ * launch, for a NULL, misaligned or mismatched argument.
+ */
+ps_status ps_kv_write_dev(ps_ctx* ctx, const ps_kv_cache* cache, const ps_kv_window* window,
+                          const ps_rows* k, const ps_rows* v, void* hip_stream);
+
+/*
+ * Read the window's rows back: the cache's values, for PS_T_E4M3 rounded to
+ * the rows' 16-bit type (exact unless the product leaves its normal range).
+ * Rows of a request that have no token, or that ps_kv_write_dev would not
+ * write, are set to zero.  Otherwise as ps_kv_write_dev.
+ */
+ps_status ps_kv_read_dev(ps_ctx* ctx, const ps_kv_cache* cache, const ps_kv_window* window,
+                         const ps_rows* k, const ps_rows* v, void* hip_stream);
+
+/*
+ * A plan: how the attention of one window is cut into work, and the memory
+ * for it (from the context; freed by ps_attend_plan_destroy, or with the
+ * context).  It serves windows of at most max_req requests and max_rows rows
+ * with n_heads query heads over n_kv_heads (a divisor of n_heads) and the
+ * given head_dim and block_tokens.
+ */
+typedef struct ps_attend_plan ps_attend_plan;
+ps_status ps_attend_plan_create(ps_ctx* ctx, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                int32_t block_tokens, int32_t max_req, int32_t max_rows,
+                                ps_attend_plan** out);
+ps_status ps_attend_plan_destroy(ps_attend_plan* plan);
+
+/*
+ * Plan a window, asynchronously on `hip_stream`: read its descriptors and
+ * pages (which may change afterwards only if the plan is made again; page
+ * numbers are read again by the attention).  Requests with the same pre_off
+ * and pre_len share one pass over that segment's keys and values where it
+ * pays.  d_flags[n_req] (may be NULL) receives 0, or PS_R_INVALID for a request whose segments leave the pool, whose
+ * chain is longer than PS_MAX_CHAIN blocks, whose ctx_tok is negative or more
+ * than the chain holds, or that needs a page outside [0, n_pages); its rows
+ * come out as empty ones.  Where row_off is not ascending within [0, n_rows],
+ * every request is flagged and the attention writes nothing.  One plan serves
+ * every layer of a step.  No allocation: it can be captured, and a replay
+ * plans what the buffers then hold.
+ */
+ps_status ps_attend_plan_dev(ps_attend_plan* plan, const ps_kv_window* window, uint32_t* d_flags,
+                             void* hip_stream);
+
+/*
+ * Attention of the planned window: for row j of request r at position p and
+ * query head h (key / value head h / (n_heads / n_kv_heads)),
+ *   out = sum over t in [0, p] of softmax_t(scale * q . k_t) v_t
+ * over the request's chain, and lse (float[n_rows * n_heads], may be NULL) the
+ * natural logarithm of the sum of exp(scale * q . k_t).  Products take the
+ * operands in q's 16-bit type (PS_T_E4M3 values are converted to it; a 16-bit
+ * cache is of q's type), sums and the softmax are in fp32, the softmax's
+ * weights are rounded to that type before they multiply v.  A row without a
+ * token gives zeros and -inf.  What lies in the pages behind a row's position
+ * does not reach it, whatever its bits.  Results do not depend on the run: the
+ * same window gives the same bits.  out must not overlap q or the cache.
+ * Asynchronous on `hip_stream`, no allocation.  The plan's memory is in use
+ * until the work is done: calls on one plan must not overlap (two graphs that
+ * may run at the same time need a plan each).  PS_E_STATE before
+ * ps_attend_plan_dev.
+ */
+ps_status ps_attend_window_dev(ps_attend_plan* plan, const ps_kv_cache* cache, const ps_rows* q,
+                               const ps_rows* out, float* lse, float scale, void* hip_stream);
+
 /* Message of the last failed call on ctx (or of ps_create when ctx is NULL). */
 const char* ps_last_error(const ps_ctx* ctx);
 

@@ -11,4 +11,5 @@ from .binding import (  # noqa: F401
     ps_table_info, results_from_device, to_device_bytes, to_device_u64, ps_apply_events,
     ps_feedback_decode, ps_feedback_output, ps_read_model, PS_EV_PREFILL_DONE,
     PS_EV_DECODE_TOKENS, PS_EV_FINISHED, PS_LOUT_WINDOW,
+    PS_T_BF16, PS_T_F16, PS_T_E4M3, KvCache, KvWindow, AttendPlan, ps_kv_write_dev, ps_kv_read_dev,
 )

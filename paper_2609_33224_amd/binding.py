@@ -47,6 +47,9 @@ assert PS_REQ_DTYPE.itemsize == 24 and PS_RESULT_DTYPE.itemsize == 20
 assert PS_EVENT_DTYPE.itemsize == 16
 PS_EV_PREFILL_DONE, PS_EV_DECODE_TOKENS, PS_EV_FINISHED = 1, 2, 3
 PS_LOUT_WINDOW = 1024
+PS_T_BF16, PS_T_F16, PS_T_E4M3 = 0, 1, 2
+PS_MAX_HEADS, PS_MAX_KV_HEADS, PS_MAX_HEAD_DIM = 1024, 128, 256
+PS_MAX_WINDOW_REQ, PS_MAX_ROWS = 8192, 1 << 20
 
 
 class PsModel(ctypes.Structure):
@@ -72,6 +75,28 @@ class PsInstances(ctypes.Structure):
         ("decoding", ctypes.c_void_p), ("queued", ctypes.c_void_p),
         ("pending_tok", ctypes.c_void_p), ("ctx_tok", ctypes.c_void_p),
     ]
+
+
+class PsKvCache(ctypes.Structure):
+    _fields_ = [
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_exp", ctypes.c_void_p),
+        ("v_exp", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("page_stride", ctypes.c_int64),
+        ("exp_page_stride", ctypes.c_int64), ("n_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32), ("block_tokens", ctypes.c_int32), ("dtype", ctypes.c_int32),
+    ]
+
+
+class PsKvWindow(ctypes.Structure):
+    _fields_ = [
+        ("pages", ctypes.c_void_p), ("reqs", ctypes.c_void_p), ("ctx_tok", ctypes.c_void_p),
+        ("row_off", ctypes.c_void_p), ("pages_len", ctypes.c_int64), ("n_pages", ctypes.c_int64),
+        ("n_req", ctypes.c_int32), ("n_rows", ctypes.c_int32),
+    ]
+
+
+class PsRows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("dtype", ctypes.c_int32)]
 
 
 class PackServeError(RuntimeError):
@@ -114,6 +139,12 @@ def load_library() -> ctypes.CDLL:
         "ps_feedback_decode": ([vp, vp, vp, vp, i32], i32),
         "ps_feedback_output": ([vp, vp, i32], i32),
         "ps_read_model": ([vp, vp, vp, vp], i32),
+        "ps_kv_write_dev": ([vp, vp, vp, vp, vp, vp], i32),
+        "ps_kv_read_dev": ([vp, vp, vp, vp, vp, vp], i32),
+        "ps_attend_plan_create": ([vp, i32, i32, i32, i32, i32, i32, ctypes.POINTER(vp)], i32),
+        "ps_attend_plan_destroy": ([vp], i32),
+        "ps_attend_plan_dev": ([vp, vp, vp, vp], i32),
+        "ps_attend_window_dev": ([vp, vp, vp, vp, vp, ctypes.c_float, vp], i32),
         "ps_set_timing": ([vp, i32], i32),
         "ps_read_kernel_timing": ([vp, ctypes.POINTER(i32), ctypes.POINTER(ctypes.c_float)], i32),
         "ps_read_timing": ([vp, ctypes.POINTER(i32), ctypes.POINTER(ctypes.c_float),
@@ -320,6 +351,176 @@ def ps_read_model(ctx) -> dict:
     return dict(gamma=g[:n.value].copy(), lout=float(lout.value))
 
 
+# ------------------------------------------------------------------ block cache
+_ROW_TYPES = {torch.bfloat16: PS_T_BF16, torch.float16: PS_T_F16}
+
+
+class KvCache:
+    """Pages of one layer: k and v are (pages, KV heads, block tokens, head
+    dim) of bfloat16, float16 or float8_e4m3fn (then with the uint8 exponents
+    k_exp and v_exp, one per page, head and slot); a page is contiguous, pages
+    may be apart.  Keeps the tensors."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_exp: Optional[torch.Tensor] = None,
+                 v_exp: Optional[torch.Tensor] = None):
+        types = {**_ROW_TYPES, torch.float8_e4m3fn: PS_T_E4M3}
+        if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype:
+            raise ValueError("k and v must be alike: (pages, KV heads, block tokens, head dim)")
+        if k.dtype not in types or not k.is_cuda or k.device != v.device:
+            raise ValueError("k and v must be device tensors of bfloat16, float16 or float8_e4m3fn")
+        pages, heads, block, dim = k.shape
+        if k.numel() and k.stride()[1:] != (block * dim, dim, 1):
+            raise ValueError("a page must be contiguous")
+        exps = (k_exp, v_exp)
+        stride = 0
+        if k.dtype == torch.float8_e4m3fn:
+            for x in exps:
+                if (x is None or x.dtype != torch.uint8 or x.shape != k.shape[:3] or x.device != k.device
+                        or x.stride() != k_exp.stride() or (x.numel() and x.stride()[1:] != (block, 1))):
+                    raise ValueError("k_exp and v_exp must be uint8 (pages, KV heads, block tokens), "
+                                     "a page contiguous")
+            stride = max(k_exp.stride(0), heads * block)
+        elif any(x is not None for x in exps):
+            raise ValueError("exponents belong to float8_e4m3fn caches")
+        self.tensors = (k, v, k_exp, v_exp)
+        self.device = k.device
+        self.dtype = k.dtype
+        self.raw = PsKvCache(k.data_ptr(), v.data_ptr(), *[x.data_ptr() if x is not None else None for x in exps],
+                             pages, max(k.stride(0), heads * block * dim), stride, heads, dim, block,
+                             types[k.dtype])
+
+    @classmethod
+    def empty(cls, n_pages: int, n_kv_heads: int, block_tokens: int, head_dim: int,
+              dtype: torch.dtype = torch.float8_e4m3fn, device="cuda") -> "KvCache":
+        """A cache of zeros."""
+        shape = (n_pages, n_kv_heads, block_tokens, head_dim)
+        bufs = [torch.zeros(shape, dtype=dtype, device=device) for _ in range(2)]
+        if dtype == torch.float8_e4m3fn:
+            bufs += [torch.ones(shape[:3], dtype=torch.uint8, device=device) for _ in range(2)]
+        return cls(*bufs)
+
+
+class KvWindow:
+    """A window over the block cache: pages (int32), the scheduler's request
+    descriptors (bytes of PS_REQ_DTYPE) into them, tokens per context and row
+    offsets (int32), all on the device.  Keeps the tensors."""
+
+    def __init__(self, pages: torch.Tensor, reqs: torch.Tensor, ctx_tok: torch.Tensor, row_off: torch.Tensor,
+                 n_req: int, n_rows: int, n_pages: int):
+        for name, t in (("pages", pages), ("ctx_tok", ctx_tok), ("row_off", row_off)):
+            if t.dtype != torch.int32:
+                raise ValueError(f"{name} must be int32")
+        if len({t.device for t in (pages, reqs, ctx_tok, row_off)}) != 1:
+            raise ValueError("the window's tensors are on different devices")
+        if (n_req < 0 or reqs.numel() * reqs.element_size() < 24 * n_req or ctx_tok.numel() < n_req
+                or row_off.numel() < (n_req + 1 if n_req else 0)):
+            raise ValueError("a window tensor is shorter than n_req says")
+        self.tensors = (pages, reqs, ctx_tok, row_off)
+        self.device = pages.device
+        self.n_req, self.n_rows = int(n_req), int(n_rows)
+        self.raw = PsKvWindow(*[_dev_ptr(t) for t in (pages, reqs, ctx_tok, row_off)], pages.numel(), int(n_pages),
+                              self.n_req, self.n_rows)
+
+
+def _same_device(*things):
+    if len({t.device for t in things if t is not None}) != 1:
+        raise ValueError("tensors on different devices")
+
+
+def _block_stream(stream, device) -> int:
+    return (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream
+
+
+def _rows(t: torch.Tensor, name: str, n_rows: int, heads: int, dim: int) -> PsRows:
+    if t.dim() != 3 or t.shape[0] < n_rows or tuple(t.shape[1:]) != (heads, dim):
+        raise ValueError(f"{name} must be (at least {n_rows} rows, {heads} heads, {dim})")
+    if t.dtype not in _ROW_TYPES or not t.is_cuda or (t.numel() and t.stride(2) != 1):
+        raise ValueError(f"{name} must be a bfloat16 or float16 device tensor, contiguous in its last axis")
+    # (an axis of one entry has no stride that matters)
+    row = t.stride(0) if t.shape[0] > 1 else max(8, heads * dim)
+    head = t.stride(1) if heads > 1 else dim
+    return PsRows(t.data_ptr(), row, head, _ROW_TYPES[t.dtype])
+
+
+def _kv_rows(call, ctx, cache: KvCache, window: KvWindow, k, v, stream) -> None:
+    _same_device(cache, window, k, v)
+    shape = (window.n_rows, cache.raw.n_kv_heads, cache.raw.head_dim)
+    rk, rv = _rows(k, "k", *shape), _rows(v, "v", *shape)
+    _check(ctx, call(ctx, ctypes.byref(cache.raw), ctypes.byref(window.raw), ctypes.byref(rk), ctypes.byref(rv),
+                     _block_stream(stream, cache.device)))
+
+
+def ps_kv_write_dev(ctx, cache: KvCache, window: KvWindow, k: torch.Tensor, v: torch.Tensor, stream=None) -> None:
+    """The window's rows k, v (rows, KV heads, head dim) into their pages,
+    quantised where the cache is float8_e4m3fn."""
+    _kv_rows(load_library().ps_kv_write_dev, ctx, cache, window, k, v, stream)
+
+
+def ps_kv_read_dev(ctx, cache: KvCache, window: KvWindow, k: torch.Tensor, v: torch.Tensor, stream=None) -> None:
+    """The window's rows of the cache into k, v (rows, KV heads, head dim)."""
+    _kv_rows(load_library().ps_kv_read_dev, ctx, cache, window, k, v, stream)
+
+
+class AttendPlan:
+    """Attention of windows over a block cache: build_dev plans a window,
+    attend_dev runs the attention of one layer (any number of times).  Keeps
+    its context (a Scorer) alive."""
+
+    def __init__(self, scorer: "Scorer", n_heads: int, n_kv_heads: int, head_dim: int, block_tokens: int,
+                 max_req: int, max_rows: int):
+        self.scorer = scorer
+        self.shape = (int(n_heads), int(head_dim))
+        self.window = None
+        h = ctypes.c_void_p()
+        self.plan = None
+        _check(scorer.ctx, load_library().ps_attend_plan_create(
+            scorer.ctx, int(n_heads), int(n_kv_heads), int(head_dim), int(block_tokens), int(max_req),
+            int(max_rows), ctypes.byref(h)))
+        self.plan = h
+
+    def close(self):
+        if self.plan and self.scorer.ctx:  # (a closed context has freed its plans)
+            load_library().ps_attend_plan_destroy(self.plan)
+        self.plan = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _handle(self):
+        if not self.plan or not self.scorer.ctx:
+            raise ValueError("the plan or its context is closed")
+        return self.plan
+
+    def build_dev(self, window: KvWindow, d_flags: Optional[torch.Tensor] = None, stream=None) -> None:
+        """Plan `window`; d_flags (uint32 or int32, one per request): PS_R_INVALID for malformed requests."""
+        if d_flags is not None and (d_flags.element_size() != 4 or d_flags.numel() < window.n_req):
+            raise ValueError("d_flags must hold 32 bits per request")
+        if d_flags is not None:
+            _same_device(window, d_flags)
+        _check(self.scorer.ctx, load_library().ps_attend_plan_dev(
+            self._handle(), ctypes.byref(window.raw), _dev_ptr(d_flags), _block_stream(stream, window.device)))
+        self.window = window
+
+    def attend_dev(self, cache: KvCache, q: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor] = None,
+                   scale: Optional[float] = None, stream=None) -> None:
+        """Attention of the planned window's rows q (rows, heads, head dim) into
+        out; lse (float32, rows x heads): log of the sum of exponentials.
+        scale: head_dim ** -0.5 where None."""
+        heads, dim = self.shape
+        n_rows = self.window.n_rows if self.window is not None else 0
+        if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape[1:]) != (heads,)
+                                or lse.dim() != 2 or lse.shape[0] < n_rows):
+            raise ValueError("lse must be float32 (rows, heads)")
+        _same_device(cache, q, out, lse, self.window)
+        rq, ro = _rows(q, "q", n_rows, heads, dim), _rows(out, "out", n_rows, heads, dim)
+        _check(self.scorer.ctx, load_library().ps_attend_window_dev(
+            self._handle(), ctypes.byref(cache.raw), ctypes.byref(rq), ctypes.byref(ro), _dev_ptr(lse),
+            float(dim ** -0.5 if scale is None else scale), _block_stream(stream, cache.device)))
+
+
 # ------------------------------------------------------------------ tensors
 def to_device_u64(a: np.ndarray, device="cuda") -> torch.Tensor:
     """uint64 host array -> int64 device tensor holding the same bits."""
@@ -411,6 +612,16 @@ class Scorer:
 
     def replay_dev(self, d_pool, pool_len, d_reqs, n_req, d_inst, d_out, stream=None) -> int:
         return ps_replay_window_dev(self.ctx, d_pool, pool_len, d_reqs, n_req, d_inst, d_out, stream)
+
+    def kv_write_dev(self, cache: KvCache, window: KvWindow, k, v, stream=None) -> None:
+        ps_kv_write_dev(self.ctx, cache, window, k, v, stream)
+
+    def kv_read_dev(self, cache: KvCache, window: KvWindow, k, v, stream=None) -> None:
+        ps_kv_read_dev(self.ctx, cache, window, k, v, stream)
+
+    def attend_plan(self, n_heads: int, n_kv_heads: int, head_dim: int, block_tokens: int, max_req: int,
+                    max_rows: int) -> AttendPlan:
+        return AttendPlan(self, n_heads, n_kv_heads, head_dim, block_tokens, max_req, max_rows)
 
     def state(self) -> dict:
         return ps_read_state(self.ctx, self.n_inst)
