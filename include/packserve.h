@@ -461,6 +461,7 @@ ps_status ps_read_model(ps_ctx* ctx, float* gamma, float* lout, int32_t* n_seg);
 #define PS_MAX_KV_HEADS 128    /* key / value heads */
 #define PS_MAX_HEAD_DIM 256
 #define PS_MAX_WINDOW_REQ 8192 /* requests of an attention plan */
+#define PS_MAX_WINDOW_CTX 1073741824 /* tokens of a request's context in the calls below */
 #define PS_MAX_ROWS 1048576    /* rows of a window in the calls below */
 
 /*
@@ -556,8 +557,8 @@ ps_status ps_attend_plan_destroy(ps_attend_plan* plan);
  * numbers are read again by the attention).  Requests with the same pre_off
  * and pre_len share one pass over that segment's keys and values where it
  * pays.  d_flags[n_req] (may be NULL) receives 0, or PS_R_INVALID for a request whose segments leave the pool, whose
- * chain is longer than PS_MAX_CHAIN blocks, whose ctx_tok is negative or more
- * than the chain holds, or that needs a page outside [0, n_pages); its rows
+ * chain is longer than PS_MAX_CHAIN blocks, whose ctx_tok is negative, more
+ * than the chain holds or above PS_MAX_WINDOW_CTX, or that needs a page outside [0, n_pages); its rows
  * come out as empty ones.  Where row_off is not ascending within [0, n_rows],
  * every request is flagged and the attention writes nothing.  One plan serves
  * every layer of a step.  No allocation: it can be captured, and a replay

@@ -1,4 +1,24 @@
 // Attention of a window's rows over their requests' chains in the block cache.
+//
+// One pass over the keys and values with the running maximum and sum of the
+// softmax, on the matrix cores: S^T = K Q^T (rows: positions, columns: rows of
+// the tile), P = exp2(S c - m c) with c = scale log2 e, O^T += V^T P^T.  In
+// this orientation a lane's column is one row of the window in both products, so the
+// maximum, the sum and the rescaling are the lane's own, and its weights are
+// in the place where the second product takes them: the k index of a matrix
+// product may be permuted, and is, so that it names the positions that the lane holds.
+//
+// A workgroup takes an equal run of the units of its head's tiles (AttendPlanDev).
+//  - A narrow tile (16 rows at most: the rows of one request that decodes) is
+//    bound by the bytes of its keys and values.  Each wave takes
+//    32 positions of its own in turn, keys straight from memory into the matrix
+//    operand, values through a wave's part of shared memory, where the
+//    transposing read turns them; the four waves' results are joined at the end.
+//  - A wide tile (128 rows: a prefix that many requests share, a prompt) is
+//    bound by the matrix cores: 64 positions are staged in shared memory for the four
+//    waves, which have 32 rows each.
+// e4m3 values are brought to the 16-bit type with their power of two as they
+// are staged (exact but for fp16's range), so one kernel serves both.
 
 #include "ps_blocks.h"
 
@@ -6,144 +26,758 @@ namespace ps {
 
 namespace {
 
-// Whether every page that a request's context needs is one of the cache's;
-// one workgroup per request.
-__global__ __launch_bounds__(256) void plan_check_kernel(AttendPlanDev p, BlockWin w, uint32_t* d_flags) {
-  const int32_t r = blockIdx.x;
-  const BlockReq q = block_req(w, r);
-  int bad = !q.ok;
-  if (q.ok) {
-    const int32_t blocks = (int32_t)(((int64_t)q.ctx + w.bt - 1) / w.bt);
-    for (int32_t b = threadIdx.x; b < blocks; b += 256) {
-      const int64_t page = w.pages[b < q.pre_len ? q.pre_off + b : q.tail_off + (b - q.pre_len)];
-      bad |= page < 0 || page >= w.n_pages;
-    }
-  }
-  bad = __syncthreads_or(bad);
-  if (threadIdx.x == 0) {
-    p.flags[r] = bad ? PS_R_INVALID : 0u;
-    if (d_flags) d_flags[r] = bad ? PS_R_INVALID : 0u;
-  }
-}
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
 
-// One workgroup: each row's request and the positions it sees.
-__global__ __launch_bounds__(1024) void plan_rows_kernel(AttendPlanDev p, BlockWin w, uint32_t* d_flags) {
-  int bad = 0;
-  for (int32_t r = threadIdx.x; r < w.n_req; r += 1024) {
-    const int32_t lo = w.row_off[r], hi = w.row_off[r + 1];
-    bad |= lo < 0 || hi < lo || hi > w.n_rows;
-  }
-  bad = __syncthreads_or(bad);
-  if (bad && d_flags)
-    for (int32_t r = threadIdx.x; r < w.n_req; r += 1024) d_flags[r] = PS_R_INVALID;
-  for (int32_t row = threadIdx.x; row < w.n_rows; row += 1024) {
-    AttendRow o{0, 0, 0, -1};
-    const int32_t r = bad || w.n_req == 0 ? -1 : block_row_req(w, row);
-    if (r >= 0) {
-      const BlockReq q = block_req(w, r);
-      o.pre_off = q.pre_off;
-      o.tail_off = q.tail_off;
-      o.pre_len = q.pre_len;
-      const int64_t lim = (int64_t)q.ctx - q.hi + row + 1;
-      o.lim = p.flags[r] || lim < 0 ? 0 : (int32_t)lim;
-    }
-    p.rows[row] = o;
-  }
+constexpr float kLn2 = 0.693147180559945309f;
+
+template <bool kF16>
+__device__ inline f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
+  if (kF16)
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
 template <bool kF16>
-__device__ inline float load16(const unsigned char* p, int64_t i) {
-  if (kF16) return (float)((const _Float16*)p)[i];
-  return __builtin_bit_cast(float, (uint32_t)((const uint16_t*)p)[i] << 16);
+__device__ inline f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
+  if (kF16)
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
 template <bool kF16>
-__device__ inline float round16(float x) {
-  if (kF16) return (float)(_Float16)x;
-  return (float)(__bf16)x;
+__device__ inline uint32_t pack(float a, float b) {
+  if (kF16) {
+    const f16x2 v = {(_Float16)a, (_Float16)b};
+    return __builtin_bit_cast(uint32_t, v);
+  }
+  const bf16x2 v = {(__bf16)a, (__bf16)b};
+  return __builtin_bit_cast(uint32_t, v);
 }
 
-template <bool kF16, bool kQuant>
-__device__ inline float load_cache(const unsigned char* p, const uint8_t* x, int64_t at, int64_t xat) {
-  if (!kQuant) return load16<kF16>(p, at);
-  const float s = __builtin_bit_cast(float, (uint32_t)x[xat] << 23);
-  return round16<kF16>(__builtin_amdgcn_cvt_f32_fp8((int)p[at], 0) * s);
+// Four e4m3 codes to 16 bits, times a power of two.
+template <bool kF16>
+__device__ inline u32x2 widen(uint32_t x, float s) {
+  u32x2 o;
+  if (kF16) {
+    o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)x, s, false));
+    o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)x, s, true));
+  } else {
+    o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)x, s, false));
+    o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)x, s, true));
+  }
+  return o;
 }
 
-// One wave per row and query head: 64 positions at a time, a lane each for
-// the scores, then lanes over the head's elements for the weighted sum.
-template <bool kF16, bool kQuant>
-__global__ __launch_bounds__(256) void attend_kernel(AttendArgs a) {
+// Half of 16 codes: 8 values.
+template <bool kF16>
+__device__ inline u32x4 widen8(uint32_t x, uint32_t y, float s) {
+  const u32x2 a = widen<kF16>(x, s), b = widen<kF16>(y, s);
+  return u32x4{a[0], a[1], b[0], b[1]};
+}
+
+// Sets infinities and NaN among 8 packed 16-bit values to 0; whether there were any.
+template <bool kF16>
+__device__ inline uint32_t clean8(u32x4& x) {
+  constexpr uint32_t lo = kF16 ? 0x7C00u : 0x7F80u, hi = lo << 16;
+  uint32_t r = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t out = ((x[i] & lo) == lo ? 0xFFFFu : 0u) | ((x[i] & hi) == hi ? 0xFFFF0000u : 0u);
+    r |= out;
+    x[i] &= ~out;
+  }
+  return r;
+}
+
+// A lane's number, anew: what is computed from it is not kept in registers from one
+// tile to the next.
+__device__ inline int fresh(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// Four rows' elements to a lane each: of 16 lanes that point to 4 rows of 16
+// elements (4 lanes a row, 4 elements a lane), lane i receives column i.
+__device__ inline u32x2 read_turned(const unsigned char* p) {
+  typedef __attribute__((address_space(3))) i16x4* lds_ptr;
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)p));
+}
+
+__device__ inline float scale_of(uint32_t x) { return __builtin_bit_cast(float, x << 23); }
+
+// The chain of a tile, with what it takes to find a position's bytes.
+struct Chain {
+  const int32_t* pages;
+  int64_t pre_off, tail_off;
+  int32_t pre_len;
+};
+
+__device__ inline int32_t block_of(const AttendArgs& a, int32_t t) {
+  return (int32_t)((__umulhi((uint32_t)t, a.bt_mul) + (uint32_t)t) >> a.bt_shift);
+}
+
+// The page of position t.  (Its number was checked when the plan was made; one that
+// has changed since is kept inside the cache.)
+__device__ inline uint32_t page_of(const AttendArgs& a, const Chain& c, int32_t t) {
+  const int32_t b = block_of(a, t);
+  const uint32_t page = (uint32_t)c.pages[b < c.pre_len ? c.pre_off + b : c.tail_off + (b - c.pre_len)];
+  return min(page, (uint32_t)a.cache.n_pages - 1u);
+}
+
+struct Spot {
+  int64_t at;  // first element of the row
+  int64_t x;   // its exponent
+};
+__device__ inline Spot spot_of(const AttendArgs& a, int32_t head, uint32_t page, int32_t t) {
+  const int32_t slot = t - block_of(a, t) * a.win.bt;
+  const int32_t r = head * a.win.bt + slot;
+  return Spot{(int64_t)page * a.cache.page_stride + (int64_t)r * a.cache.dim, (int64_t)page * a.cache.exp_stride + r};
+}
+
+// One piece of a tile: positions [ta, tb) for its rows.
+struct Piece {
+  Chain chain;
+  int32_t p0, row0, rows;
+  int32_t ta, tb;
+  int32_t slot;  // first row of its partial results, -1: the result itself
+  int32_t head;
+  float c;       // |scale| log2 e
+  uint32_t neg;  // sign bits that turn q where scale is negative
+};
+
+// Row r of the tile (of the window's rows in their order x the group's heads).
+struct RowAt {
+  int32_t place, head;
+};
+__device__ inline RowAt row_at(const AttendArgs& a, const Piece& p, int32_t r) {
+  const int32_t x = p.row0 + r, t = x / a.ratio;
+  return RowAt{p.p0 + t, p.head * a.ratio + (x - t * a.ratio)};
+}
+
+// Elements d .. d + 3 of position t's value row, infinities and NaN as they
+// are and everything else 0.
+template <bool kF16, bool kQ8>
+__device__ inline f32x4 odd_values(const AttendArgs& a, const Piece& p, int32_t t, int32_t d) {
+  const Spot s = spot_of(a, p.head, page_of(a, p.chain, t), t);
+  u32x2 x;
+  if (kQ8) x = widen<kF16>(*(const uint32_t*)(a.cache.v + s.at + d), scale_of(a.cache.vx[s.x]));
+  else x = *(const u32x2*)(a.cache.v + 2 * (s.at + d));
+  f32x4 o;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t h = i & 1 ? x[i >> 1] >> 16 : x[i >> 1] & 0xFFFFu;
+    const float f = kF16 ? (float)__builtin_bit_cast(_Float16, (uint16_t)h) : __builtin_bit_cast(float, h << 16);
+    o[i] = __builtin_isfinite(f) ? 0.0f : f;
+  }
+  return o;
+}
+
+// Eight elements of a row of q, from element d.
+__device__ inline u32x4 load_q(const AttendArgs& a, const Piece& p, int32_t r, int32_t d) {
+  u32x4 x = {0, 0, 0, 0};
+  if (r < p.rows && d < a.cache.dim) {
+    const RowAt at = row_at(a, p, r);
+    x = *(const u32x4*)(a.q.data + 2 * ((int64_t)a.plan.row[at.place] * a.q.row + (int64_t)at.head * a.q.head + d));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] ^= p.neg;
+  }
+  return x;
+}
+
+// Four results of a row, from element d: written out, or kept as a partial result.
+template <bool kF16>
+__device__ inline void put4(const AttendArgs& a, const Piece& p, int32_t r, int32_t d, f32x4 o, float inv) {
+  if (d >= a.cache.dim) return;
+  if (p.slot >= 0) {
+    const int64_t at = (int64_t)p.head * a.plan.slot_rows + p.slot + r;
+    *(f32x4*)(a.plan.part + at * a.cache.dim + d) = o;
+    return;
+  }
+  const RowAt w = row_at(a, p, r);
+  const u32x2 x = {pack<kF16>(o[0] * inv, o[1] * inv), pack<kF16>(o[2] * inv, o[3] * inv)};
+  *(u32x2*)(a.out.data + 2 * ((int64_t)a.plan.row[w.place] * a.out.row + (int64_t)w.head * a.out.head + d)) = x;
+}
+
+// A row's maximum (of scores) and sum, likewise; returns what its results are
+// multiplied by where they are final.
+__device__ inline float put_ml(const AttendArgs& a, const Piece& p, int32_t r, float m, float l, bool write) {
+  const float mc = m == -INFINITY ? -INFINITY : m * p.c;
+  if (p.slot >= 0) {
+    if (write) a.plan.part_ml[(int64_t)p.head * a.plan.slot_rows + p.slot + r] = float2{mc, l};
+    return 1.0f;
+  }
+  const RowAt w = row_at(a, p, r);
+  const bool empty = a.plan.lim[w.place] <= 0;
+  if (write && a.lse)
+    a.lse[(int64_t)a.plan.row[w.place] * a.heads + w.head] =
+        empty ? -INFINITY : __builtin_fmaf(mc, kLn2, __logf(l));
+  return empty ? 0.0f : 1.0f / l;
+}
+
+// ------------------------------------------------------------------ narrow
+
+// Shared memory of a wave's 32 positions of values: DP elements a row, chunks
+// of 8 at chunk ^ 2 (row % 8), so that neither the rows' writes nor the turned reads
+// of 16 rows meet in a bank more than their size makes them.
+template <int DP>
+__device__ inline int vswz(int row, int chunk) {
+  return row * (DP * 2) + ((chunk ^ ((row & 7) << 1)) & (DP / 8 - 1)) * 16;
+}
+
+template <bool kF16, bool kQ8, int DP, int RB>
+__device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char* smem, float2* ml) {
+  constexpr int kSteps = DP / 32;                     // of the first product
+  constexpr int kLoads = kQ8 ? DP / 64 : DP / 32;     // 16-byte loads per lane and 16 positions
+  constexpr int kDB = DP / 16;                        // blocks of the second product
+  const int lane = fresh(threadIdx.x & 63), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 15, g = lane >> 4;
+  const int D = a.cache.dim;
+  unsigned char* vs = smem + wave * 32 * DP * 2;
+
+  u32x4 q[RB][kSteps];
+  int32_t lim[RB], least = INT32_MAX;
+#pragma unroll
+  for (int b = 0; b < RB; ++b) {
+    const int32_t r = b * 16 + col;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+      q[b][s] = load_q(a, p, r, kQ8 ? 64 * (s >> 1) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g);
+    lim[b] = r < p.rows ? a.plan.lim[row_at(a, p, r).place] : INT32_MAX;
+    least = min(least, lim[b]);
+  }
+  for (int o = 8; o > 0; o >>= 1) least = min(least, __shfl_xor(least, o, 64));
+
+  f32x4 acc[RB][kDB];
+  float m[RB], l[RB];
+#pragma unroll
+  for (int b = 0; b < RB; ++b) {
+    m[b] = -INFINITY;
+    l[b] = 0;
+#pragma unroll
+    for (int k = 0; k < kDB; ++k) acc[b][k] = f32x4{0, 0, 0, 0};
+  }
+
+  const int32_t last = p.tb - 1;
+  uint32_t page[2];
+  u32x4 kr[2][kLoads], vr[2][kLoads];
+  uint32_t kx[2], vx[2];
+  auto pages = [&](int32_t t) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) page[h] = page_of(a, p.chain, min(t + 16 * h + col, last));
+  };
+  auto loads = [&](int32_t t) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const Spot s = spot_of(a, p.head, page[h], min(t + 16 * h + col, last));
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        // (where the head has fewer elements than DP, its last ones once more: they
+        // meet zeros of q, and results that nobody reads)
+        const int d = kQ8 ? min(64 * i + 16 * g, D - 16) : min(32 * i + 8 * g, D - 8);
+        const int64_t at = kQ8 ? s.at + d : 2 * (s.at + d);
+        kr[h][i] = *(const u32x4*)(a.cache.k + at);
+        vr[h][i] = *(const u32x4*)(a.cache.v + at);
+      }
+      if (kQ8) {
+        kx[h] = a.cache.kx[s.x];
+        vx[h] = a.cache.vx[s.x];
+      }
+    }
+  };
+
+  int32_t t = p.ta + 32 * wave;
+  if (t < p.tb) {
+    pages(t);
+    loads(t);
+    pages(t + 128);
+  }
+  for (; t < p.tb; t += 128) {
+    // Values into shared memory.  Where a row may not see all of the 32, their
+    // infinities and NaN are taken out, since a weight of 0 would not take them
+    // away; the rows that see them get them below.
+    const bool masked = t + 32 > p.tb || t + 32 > least;  // (the same for the wave)
+    uint32_t odd = 0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int row = 16 * h + col;
+        if (kQ8) {
+          const float s = scale_of(vx[h]);
+          u32x4 x = widen8<kF16>(vr[h][i][0], vr[h][i][1], s), y = widen8<kF16>(vr[h][i][2], vr[h][i][3], s);
+          if (masked) {
+            odd |= clean8<kF16>(x);
+            odd |= clean8<kF16>(y);
+          }
+          *(u32x4*)(vs + vswz<DP>(row, 8 * i + 2 * g)) = x;
+          *(u32x4*)(vs + vswz<DP>(row, 8 * i + 2 * g + 1)) = y;
+        } else {
+          if (masked) odd |= clean8<kF16>(vr[h][i]);
+          *(u32x4*)(vs + vswz<DP>(row, 4 * i + g)) = vr[h][i];
+        }
+      }
+    // scores: position 16 h + 4 g + i of the 32, row b * 16 + col
+    f32x4 s[RB][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int b = 0; b < RB; ++b) s[b][h] = f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int st = 0; st < kSteps; ++st) {
+        u32x4 ka;
+        if (kQ8) {
+          const u32x4 x = kr[h][st >> 1];
+          ka = st & 1 ? widen8<kF16>(x[2], x[3], scale_of(kx[h])) : widen8<kF16>(x[0], x[1], scale_of(kx[h]));
+        } else {
+          ka = kr[h][st % kLoads];
+        }
+#pragma unroll
+        for (int b = 0; b < RB; ++b) s[b][h] = mfma16<kF16>(ka, q[b][st], s[b][h]);
+      }
+    }
+    if (t + 128 < p.tb) {
+      loads(t + 128);
+      pages(t + 256);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+
+    if (masked) {
+#pragma unroll
+      for (int b = 0; b < RB; ++b)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (t + 16 * h + 4 * g + i >= min(lim[b], p.tb)) s[b][h][i] = -INFINITY;
+    }
+    u32x4 pr[RB];
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+      float top = s[b][0][0];
+#pragma unroll
+      for (int i = 1; i < 8; ++i) top = fmaxf(top, s[b][i >> 2][i & 3]);
+      top = fmaxf(top, __shfl_xor(top, 16, 64));
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      const float nm = fmaxf(m[b], top), mc = nm == -INFINITY ? 0.0f : nm * p.c;
+      const float f = __builtin_amdgcn_exp2f(__builtin_fmaf(m[b], p.c, -mc));
+      m[b] = nm;
+      float e[8], sum = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i >> 2][i & 3], p.c, -mc));
+        sum += e[i];
+      }
+      l[b] = __builtin_fmaf(l[b], f, sum);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) pr[b][i] = pack<kF16>(e[2 * i], e[2 * i + 1]);
+#pragma unroll
+      for (int k = 0; k < kDB; ++k) acc[b][k] *= f;
+    }
+    // lane i of 16: row 4 g + i / 4, elements 16 k + 4 (i % 4) ..
+    auto turned = [&](int k) {
+      const int row = 4 * g + (col >> 2), half = (col & 2) >> 1, off = 8 * (col & 1);
+      const u32x2 x = read_turned(vs + vswz<DP>(row, 2 * k + half) + off);
+      const u32x2 y = read_turned(vs + vswz<DP>(16 + row, 2 * k + half) + off);
+      return u32x4{x[0], x[1], y[0], y[1]};
+    };
+    if (masked && __any(odd != 0))
+#pragma unroll 1
+      for (int32_t o = t; o < min(t + 32, p.tb); ++o)
+#pragma unroll
+        for (int k = 0; k < kDB; ++k) {
+          const f32x4 x = odd_values<kF16, kQ8>(a, p, o, min(16 * k + fresh(4 * g), D - 4));
+#pragma unroll
+          for (int b = 0; b < RB; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[b][k][i] += o < lim[b] ? x[i] : 0.0f;
+        }
+#pragma unroll
+    for (int k = 0; k < kDB; ++k) {
+      const u32x4 va = turned(k);
+#pragma unroll
+      for (int b = 0; b < RB; ++b) acc[b][k] = mfma16<kF16>(va, pr[b], acc[b][k]);
+    }
+  }
+
+  // the four waves' results: waves 2 and 3 to 0 and 1, then 1 to 0
+#pragma unroll
+  for (int b = 0; b < RB; ++b) {
+    l[b] += __shfl_xor(l[b], 16, 64);
+    l[b] += __shfl_xor(l[b], 32, 64);
+    if (g == 0) ml[wave * kNarrowRows + b * 16 + col] = float2{m[b], l[b]};
+  }
+  __syncthreads();
+#pragma unroll
+  for (int b = 0; b < RB; ++b) {
+    float top = -INFINITY;
+    for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[w * kNarrowRows + b * 16 + col].x);
+    const float mc = top == -INFINITY ? 0.0f : top * p.c;
+    float sum = 0;
+    for (int w = 0; w < 4; ++w) {
+      const float2 x = ml[w * kNarrowRows + b * 16 + col];
+      sum += x.y * __builtin_amdgcn_exp2f(__builtin_fmaf(x.x, p.c, -mc));
+    }
+    const float f = __builtin_amdgcn_exp2f(__builtin_fmaf(m[b], p.c, -mc));
+#pragma unroll
+    for (int k = 0; k < kDB; ++k) acc[b][k] *= f;
+    m[b] = top;
+    l[b] = sum;
+  }
+  f32x4* os = (f32x4*)smem;
+  for (int from = 2; from > 0; from >>= 1) {
+    if (wave >= from && wave < 2 * from)
+#pragma unroll
+      for (int b = 0; b < RB; ++b)
+#pragma unroll
+        for (int k = 0; k < kDB; ++k) os[(((wave - from) * RB + b) * kDB + k) * 64 + lane] = acc[b][k];
+    __syncthreads();
+    if (wave < from)
+#pragma unroll
+      for (int b = 0; b < RB; ++b)
+#pragma unroll
+        for (int k = 0; k < kDB; ++k) acc[b][k] += os[((wave * RB + b) * kDB + k) * 64 + lane];
+    __syncthreads();
+  }
+  if (wave == 0) {
+    const int at = fresh(lane), d0 = 4 * (at >> 4);
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+      const int32_t r = b * 16 + (at & 15);
+      if (r < p.rows) {
+        const float inv = put_ml(a, p, r, m[b], l[b], d0 == 0);
+#pragma unroll
+        for (int k = 0; k < kDB; ++k) put4<kF16>(a, p, r, 16 * k + d0, acc[b][k], inv);
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------ wide
+
+template <int DP>
+__device__ inline int kswz(int row, int chunk) {
+  return row * (DP * 2) + ((chunk ^ row) & (DP / 8 - 1)) * 16;
+}
+
+// Positions of a wide step: 64, or 32 where a row's registers leave no room.
+constexpr int wide_positions(int DP) { return DP <= 128 ? 64 : 32; }
+
+template <bool kF16, bool kQ8, int DP>
+__device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* smem, int32_t* odd_at) {
+  constexpr int kSteps = DP / 16;
+  constexpr int kTok = wide_positions(DP);
+  constexpr int kPer = 256 / kTok;                               // threads that stage a row
+  constexpr int kLoads = (kQ8 ? DP / 16 : DP / 8) / kPer;  // 16-byte loads per thread
+  constexpr int kDB = DP / 32;
+  constexpr int kTile = kTok * DP * 2;
+  const int lane = fresh(threadIdx.x & 63), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 31, hb = lane >> 5;
+  const int D = a.cache.dim;
+  const int32_t r = wave * 32 + col;
+  const bool idle = wave * 32 >= p.rows;
+
+  u32x4 q[kSteps];
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s) q[s] = load_q(a, p, r, 16 * s + 8 * hb);
+  const int32_t lim = r < p.rows ? a.plan.lim[row_at(a, p, r).place] : INT32_MAX;
+  int32_t least = lim;
+  for (int o = 16; o > 0; o >>= 1) least = min(least, __shfl_xor(least, o, 64));
+
+  f32x16 acc[kDB];
+#pragma unroll
+  for (int k = 0; k < kDB; ++k)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[k][i] = 0;
+  float m = -INFINITY, l = 0;
+
+  // staging: thread x takes row x / kPer of the positions, chunks x % kPer + kPer i
+  const int srow = wave * (64 / kPer) + lane / kPer, sc = lane % kPer;
+  const int32_t last = p.tb - 1;
+  uint32_t page;
+  u32x4 kr[kLoads], vr[kLoads];
+  uint32_t kx = 0, vx = 0;
+  auto pages = [&](int32_t t) { page = page_of(a, p.chain, min(t + srow, last)); };
+  auto loads = [&](int32_t t) {
+    const Spot s = spot_of(a, p.head, page, min(t + srow, last));
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int d = kQ8 ? min(16 * (kPer * i + sc), D - 16) : min(8 * (kPer * i + sc), D - 8);  // (as in the narrow kernel)
+      const int64_t at = kQ8 ? s.at + d : 2 * (s.at + d);
+      kr[i] = *(const u32x4*)(a.cache.k + at);
+      vr[i] = *(const u32x4*)(a.cache.v + at);
+    }
+    if (kQ8) {
+      kx = a.cache.kx[s.x];
+      vx = a.cache.vx[s.x];
+    }
+  };
+  // (of one request's rows the first sees least; those of a shared prefix see all of it)
+  const int32_t least_of_all = a.plan.lim[row_at(a, p, 0).place];
+  auto stage = [&](int buf, int32_t t) {
+    const bool masked = t + kTok > p.tb || t + kTok > least_of_all;
+    uint32_t odd = 0;
+    unsigned char* ks = smem + buf * 2 * kTile;
+    unsigned char* vs = ks + kTile;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      if (kQ8) {
+        const float sk = scale_of(kx), sv = scale_of(vx);
+        const int ch = 2 * (kPer * i + sc);
+        *(u32x4*)(ks + kswz<DP>(srow, ch)) = widen8<kF16>(kr[i][0], kr[i][1], sk);
+        *(u32x4*)(ks + kswz<DP>(srow, ch + 1)) = widen8<kF16>(kr[i][2], kr[i][3], sk);
+        u32x4 x = widen8<kF16>(vr[i][0], vr[i][1], sv), y = widen8<kF16>(vr[i][2], vr[i][3], sv);
+        if (masked) {  // (as in the narrow kernel)
+          odd |= clean8<kF16>(x);
+          odd |= clean8<kF16>(y);
+        }
+        *(u32x4*)(vs + vswz<DP>(srow, ch)) = x;
+        *(u32x4*)(vs + vswz<DP>(srow, ch + 1)) = y;
+      } else {
+        if (masked) odd |= clean8<kF16>(vr[i]);
+        *(u32x4*)(ks + kswz<DP>(srow, kPer * i + sc)) = kr[i];
+        *(u32x4*)(vs + vswz<DP>(srow, kPer * i + sc)) = vr[i];
+      }
+    }
+    if (odd) odd_at[buf] = t;  // (a value left by another piece only costs a look)
+  };
+
+  pages(p.ta);
+  loads(p.ta);
+  pages(p.ta + kTok);
+  stage(0, p.ta);
+  __syncthreads();
+  int buf = 0;
+  for (int32_t t = p.ta; t < p.tb; t += kTok, buf ^= 1) {
+    const bool more = t + kTok < p.tb;
+    if (more) {
+      loads(t + kTok);
+      pages(t + 2 * kTok);
+    }
+    if (!idle) {
+      const unsigned char* ks = smem + buf * 2 * kTile;
+      const unsigned char* vs = ks + kTile;
+      // scores: position 32 b + 8 (i / 4) + 4 hb + i % 4 of the tile's
+      f32x16 s[kTok / 32];
+#pragma unroll
+      for (int b = 0; b < kTok / 32; ++b) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[b][i] = 0;
+#pragma unroll
+        for (int st = 0; st < kSteps; ++st)
+          s[b] = mfma32<kF16>(*(const u32x4*)(ks + kswz<DP>(32 * b + col, 2 * st + hb)), q[st], s[b]);
+      }
+      const bool masked = t + kTok > p.tb || t + kTok > least;
+      if (masked) {
+#pragma unroll
+        for (int b = 0; b < kTok / 32; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (t + 32 * b + 8 * (i >> 2) + 4 * hb + (i & 3) >= min(lim, p.tb)) s[b][i] = -INFINITY;
+      }
+      float top = s[0][0];
+#pragma unroll
+      for (int i = 1; i < kTok / 2; ++i) top = fmaxf(top, s[i >> 4][i & 15]);
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      const float nm = fmaxf(m, top), mc = nm == -INFINITY ? 0.0f : nm * p.c;
+      if (__any(nm > m)) {  // (a factor of 1 otherwise)
+        const float f = __builtin_amdgcn_exp2f(__builtin_fmaf(m, p.c, -mc));
+        l *= f;
+#pragma unroll
+        for (int k = 0; k < kDB; ++k) acc[k] *= f;
+      }
+      m = nm;
+      u32x4 pr[kTok / 16];
+      float sum = 0;
+#pragma unroll
+      for (int x = 0; x < kTok / 16; ++x)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int at = (x & 1) * 8 + 2 * i;
+          const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x >> 1][at], p.c, -mc));
+          const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x >> 1][at + 1], p.c, -mc));
+          sum += e0 + e1;
+          pr[x][i] = pack<kF16>(e0, e1);
+        }
+      l += sum;
+      // lane: element 32 k + col; positions 16 x + 8 jj + 4 hb ..
+      auto turned = [&](int x, int k) {
+        const int i = lane & 15, sub = (lane >> 4) & 1;
+        const int row = 16 * x + 4 * hb + (i >> 2), ch = 4 * k + 2 * sub + ((i & 2) >> 1), off = 8 * (i & 1);
+        const u32x2 y0 = read_turned(vs + vswz<DP>(row, ch) + off);
+        const u32x2 y1 = read_turned(vs + vswz<DP>(row + 8, ch) + off);
+        return u32x4{y0[0], y0[1], y1[0], y1[1]};
+      };
+      if (masked && odd_at[buf] == t)
+#pragma unroll 1
+        for (int32_t o = t; o < min(t + kTok, p.tb); ++o)
+#pragma unroll
+          for (int k = 0; k < 4 * kDB; ++k) {
+            const f32x4 x = odd_values<kF16, kQ8>(a, p, o, min(8 * k + fresh(4 * hb), D - 4));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[k >> 2][4 * (k & 3) + i] += o < lim ? x[i] : 0.0f;
+          }
+#pragma unroll
+      for (int x = 0; x < kTok / 16; ++x)
+#pragma unroll
+        for (int k = 0; k < kDB; ++k) acc[k] = mfma32<kF16>(turned(x, k), pr[x], acc[k]);
+    }
+    if (more) stage(buf ^ 1, t + kTok);
+    __syncthreads();
+  }
+  l += __shfl_xor(l, 32, 64);
+  const int at = fresh(lane), d0 = 4 * (at >> 5);
+  const int32_t ro = wave * 32 + (at & 31);
+  if (ro < p.rows) {
+    const float inv = put_ml(a, p, ro, m, l, d0 == 0);
+#pragma unroll
+    for (int k = 0; k < kDB; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        put4<kF16>(a, p, ro, 32 * k + 8 * i + d0,
+                   f32x4{acc[k][4 * i], acc[k][4 * i + 1], acc[k][4 * i + 2], acc[k][4 * i + 3]}, inv);
+  }
+}
+
+// The last of n tiles that begins at or before unit u, by the whole wave.
+__device__ inline int32_t tile_at(const int64_t* begin, int32_t n, int64_t u) {
+  const int lane = threadIdx.x & 63;
+  int32_t a = 0, b = n;  // begin[a] <= u
+  while (b - a > 1) {
+    const int32_t step = (b - a + 63) / 64, i = a + lane * step;
+    const int32_t hits = __popcll(__ballot(i < b && begin[i] <= u));
+    a += (hits - 1) * step;
+    b = min(b, a + step);
+  }
+  return a;
+}
+
+template <bool kF16, bool kQ8, int DP>
+__global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_kernel(AttendArgs a) {
+  __shared__ __align__(16) unsigned char smem[4 * wide_positions(DP) * DP * 2];
+  __shared__ float2 ml[4 * kNarrowRows];
+  __shared__ int32_t odd_at[2];
+  if (threadIdx.x < 2) odd_at[threadIdx.x] = -1;
+  __syncthreads();
+  const int32_t head = blockIdx.x % a.cache.heads, j = blockIdx.x / a.cache.heads;
+  const AttendHead& h = *a.plan.head;
+  const float c = a.scale * 1.44269504088896341f;
+  Piece p;
+  p.chain.pages = a.win.pages;
+  p.head = head;
+  p.c = fmaxf(fabsf(c), 1.17549435e-38f);  // (not 0: it multiplies infinities)
+  p.neg = c < 0 ? 0x80008000u : 0u;
+  for (int kind = 0; kind < 2; ++kind) {
+    const int32_t n = h.groups[kind];
+    if (j >= n) continue;
+    const int64_t units = h.units[kind];
+    int64_t u = units * j / n;
+    const int64_t end = units * (j + 1) / n;
+    for (int32_t k = tile_at(a.plan.begin[kind], h.n_tiles[kind], u); u < end; ++k) {
+      const AttendTile t = a.plan.tiles[kind][k];
+      const int64_t from = u - a.plan.begin[kind][k];
+      const int64_t len = max(0, (t.t1 - t.t0 + kUnit - 1) / kUnit), to = min(len, from + (end - u));
+      if (to <= from) continue;  // (a tile of no positions)
+      p.chain.pre_off = t.pre_off;
+      p.chain.tail_off = t.tail_off;
+      p.chain.pre_len = t.pre_len;
+      p.p0 = t.p0;
+      p.row0 = t.row0;
+      p.rows = t.rows;
+      p.ta = t.t0 + (int32_t)(from * kUnit);
+      p.tb = (int32_t)min((int64_t)t.t1, t.t0 + to * kUnit);
+      p.slot = t.slot < 0 ? -1 : t.slot + (j - t.first) * t.rows;
+      if (kind == 0) wide_piece<kF16, kQ8, DP>(a, p, smem, odd_at);
+      else narrow_piece<kF16, kQ8, DP, kNarrowRows / 16>(a, p, smem, ml);
+      u += to - from;
+    }
+  }
+}
+
+// Joins the partial results of each row and query head, one wave each, and
+// writes the rows that nothing was computed for.
+template <bool kF16>
+__global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
   const int lane = threadIdx.x & 63;
   const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int32_t row = (int32_t)(id / a.heads), h = (int32_t)(id % a.heads);
-  if (row >= a.win.n_rows) return;
-  const AttendRow m = a.plan.rows[row];
-  if (m.lim < 0) return;
-  const BlockCache& c = a.cache;
-  const int32_t kvh = h / (a.heads / c.heads), D = c.dim;
-  const unsigned char* q = a.q.data + 2 * (row * a.q.row + h * a.q.head);
-  float acc[4] = {0, 0, 0, 0}, mx = -INFINITY, l = 0;
-  for (int32_t t0 = 0; t0 < m.lim; t0 += 64) {
-    const int32_t n = min(64, m.lim - t0);
-    int64_t at = 0, xat = 0;
-    float s = -INFINITY;
-    if (lane < n) {
-      const int32_t t = t0 + lane, b = t / c.bt;
-      const int64_t page = min((uint32_t)c.n_pages - 1u,
-                               (uint32_t)a.win.pages[b < m.pre_len ? m.pre_off + b : m.tail_off + (b - m.pre_len)]);
-      const int64_t r = (int64_t)kvh * c.bt + (t - b * c.bt);
-      at = page * c.page_stride + r * D;
-      xat = page * c.exp_stride + r;
-      float d = 0;
-      for (int e = 0; e < D; ++e) d += load16<kF16>(q, e) * load_cache<kF16, kQuant>(c.k, c.kx, at + e, xat);
-      s = d * a.scale;
-    }
-    float top = s;
-    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-    const float nm = fmaxf(mx, top), safe = nm == -INFINITY ? 0.0f : nm;
-    const float w = expf(s - safe), f = expf(mx - safe);
-    float sum = w;
-    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-    l = l * f + sum;
-    mx = nm;
-    const float wr = round16<kF16>(w);
-    for (int g = 0; g < 4; ++g) acc[g] *= f;
-    for (int j = 0; j < n; ++j) {
-      const float pw = __shfl(wr, j, 64);
-      const int64_t vat = __shfl((long long)at, j, 64), vx = __shfl((long long)xat, j, 64);
-      for (int g = 0; g < 4; ++g)
-        if (g * 64 + lane < D) acc[g] += pw * load_cache<kF16, kQuant>(c.v, c.vx, vat + g * 64 + lane, vx);
+  const int32_t at = (int32_t)(id / a.heads), qh = (int32_t)(id % a.heads);
+  if (at >= a.plan.head->n_order) return;
+  const int32_t head = qh / a.ratio, sub = qh - head * a.ratio, i = a.plan.place[at], lead = a.plan.lead[i];
+  int64_t from[2];
+  int32_t n[2] = {0, 0}, step[2] = {0, 0};
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int32_t si = k == 0 ? 2 * i + 1 : 2 * lead;
+    if (si < 0) continue;
+    const AttendSeg& s = a.plan.segs[si];
+    if (s.tiles == 0) continue;
+    const int32_t x = (at - s.p0) * a.ratio + sub, ti = s.wide ? x / kWideRows : 0;
+    const AttendTile& t = a.plan.tiles[s.wide ? 0 : 1][s.tile0 + ti];
+    if (t.pieces > 0 && t.slot < 0) return;  // written out already
+    n[k] = t.pieces;
+    step[k] = t.rows;
+    from[k] = (int64_t)head * a.plan.slot_rows + t.slot + (x - t.row0);
+  }
+  const int32_t total = n[0] + n[1];
+  auto slot = [&](int32_t j) { return j < n[0] ? from[0] + (int64_t)j * step[0] : from[1] + (int64_t)(j - n[0]) * step[1]; };
+  float top = -INFINITY;
+  for (int32_t j = lane; j < total; j += 64) top = fmaxf(top, a.plan.part_ml[slot(j)].x);
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+  const float mc = top == -INFINITY ? 0.0f : top;
+  const int32_t D = a.cache.dim, d = 4 * lane;
+  f32x4 acc = {0, 0, 0, 0};
+  float l = 0;
+  for (int32_t j = 0; j < total; ++j) {
+    const int64_t s = slot(j);
+    const float2 x = a.plan.part_ml[s];
+    const float f = __builtin_amdgcn_exp2f(x.x - mc);
+    l = __builtin_fmaf(x.y, f, l);
+    if (d < D) {
+      const f32x4 o = *(const f32x4*)(a.plan.part + s * D + d);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(o[e], f, acc[e]);
     }
   }
-  const float inv = m.lim == 0 ? 0.0f : 1.0f / l;
-  for (int g = 0; g < 4; ++g) {
-    const int e = g * 64 + lane;
-    if (e >= D) continue;
-    const int64_t at = row * a.out.row + h * a.out.head + e;
-    const float o = m.lim == 0 ? 0.0f : acc[g] * inv;
-    if (kF16) ((_Float16*)a.out.data)[at] = (_Float16)o;
-    else ((__bf16*)a.out.data)[at] = (__bf16)o;
+  const bool empty = a.plan.lim[at] <= 0;
+  const float inv = 1.0f / l;
+  const int64_t row = a.plan.row[at];
+  if (d < D) {
+    u32x2 x = {0, 0};
+    if (!empty) x = u32x2{pack<kF16>(acc[0] * inv, acc[1] * inv), pack<kF16>(acc[2] * inv, acc[3] * inv)};
+    *(u32x2*)(a.out.data + 2 * (row * a.out.row + (int64_t)qh * a.out.head + d)) = x;
   }
-  if (a.lse && lane == 0) a.lse[(int64_t)row * a.heads + h] = m.lim == 0 ? -INFINITY : mx + logf(l);
+  if (a.lse && lane == 0) a.lse[row * a.heads + qh] = empty ? -INFINITY : __builtin_fmaf(top, kLn2, __logf(l));
+}
+
+template <bool kF16, bool kQ8>
+void launch(const AttendArgs& a, dim3 grid, hipStream_t s) {
+  if (a.cache.dim <= 64) hipLaunchKernelGGL((attend_kernel<kF16, kQ8, 64>), grid, dim3(256), 0, s, a);
+  else if (a.cache.dim <= 128) hipLaunchKernelGGL((attend_kernel<kF16, kQ8, 128>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((attend_kernel<kF16, kQ8, 256>), grid, dim3(256), 0, s, a);
 }
 
 }  // namespace
 
 }  // namespace ps
 
-hipError_t ps_launch_attend_plan(const ps::AttendPlanDev& p, const ps::BlockWin& w, uint32_t* d_flags, hipStream_t s) {
-  if (w.n_req > 0) hipLaunchKernelGGL(ps::plan_check_kernel, dim3(w.n_req), dim3(256), 0, s, p, w, d_flags);
-  hipLaunchKernelGGL(ps::plan_rows_kernel, dim3(1), dim3(1024), 0, s, p, w, d_flags);
-  return hipGetLastError();
-}
+int32_t ps_attend_per_cu(int32_t dim) { return dim <= 128 ? 2 : 1; }
 
 hipError_t ps_launch_attend(const ps::AttendArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)(((int64_t)a.win.n_rows * a.heads + 3) / 4)), block(256);
+  const dim3 grid((unsigned)(a.plan.groups * a.cache.heads));
+  const dim3 join((unsigned)(((int64_t)a.win.n_rows * a.heads + 3) / 4));
   const bool f16 = a.q.dtype == PS_T_F16, quant = a.cache.dtype == PS_T_E4M3;
-  if (f16 && quant) hipLaunchKernelGGL((ps::attend_kernel<true, true>), grid, block, 0, s, a);
-  else if (f16) hipLaunchKernelGGL((ps::attend_kernel<true, false>), grid, block, 0, s, a);
-  else if (quant) hipLaunchKernelGGL((ps::attend_kernel<false, true>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((ps::attend_kernel<false, false>), grid, block, 0, s, a);
+  if (f16 && quant) ps::launch<true, true>(a, grid, s);
+  else if (f16) ps::launch<true, false>(a, grid, s);
+  else if (quant) ps::launch<false, true>(a, grid, s);
+  else ps::launch<false, false>(a, grid, s);
+  if (f16) hipLaunchKernelGGL(ps::join_kernel<true>, join, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(ps::join_kernel<false>, join, dim3(256), 0, s, a);
   return hipGetLastError();
 }

@@ -54,7 +54,7 @@ __host__ __device__ inline BlockReq block_req(const BlockWin& w, int32_t r) {
   q.ok = d.pre_len >= 0 && d.tail_len >= 0 && d.pre_off >= 0 && d.tail_off >= 0 && d.pre_len <= w.pages_len &&
          d.tail_len <= w.pages_len && d.pre_off <= w.pages_len - d.pre_len && d.tail_off <= w.pages_len - d.tail_len &&
          (int64_t)d.pre_len + d.tail_len <= PS_MAX_CHAIN && q.ctx >= 0 &&
-         q.ctx <= ((int64_t)d.pre_len + d.tail_len) * w.bt;
+         q.ctx <= ((int64_t)d.pre_len + d.tail_len) * w.bt && q.ctx <= PS_MAX_WINDOW_CTX;
   return q;
 }
 
@@ -88,16 +88,73 @@ __host__ __device__ inline bool block_locate(const BlockWin& w, int32_t row, boo
   return *page >= 0 && *page < w.n_pages;
 }
 
-// What the attention of one row needs.
-struct AttendRow {
-  int64_t pre_off, tail_off;
+// ---- the attention's plan
+//
+// A segment is a run of a chain's positions [t0, t1) and the window's rows
+// that attend over it: a prefix that several requests share with the rows of
+// all of them, or what is left of one request's chain with its own rows.  Its
+// rows (row of the window x query head of the group, row-major) are cut into
+// tiles; a tile is wide (up to kWideRows rows) or narrow (all rows of a segment of
+// kNarrowRows at most).  The tiles' positions, in units of kUnit, laid end
+// to end are dealt in equal runs to the workgroups of each key / value head,
+// so that a tile may be cut into pieces; pieces and shared segments leave
+// partial results, which a second kernel joins.
+constexpr int kUnit = 64;
+constexpr int kWideRows = 128;
+constexpr int kNarrowRows = 16;
+constexpr int kShareMinTokens = 64;  // of a prefix
+constexpr int kShareMaxRows = 64;    // of a member (or one row of all its heads)
+
+struct AttendSeg {
+  int64_t pre_off, tail_off;  // the chain of one of its requests
   int32_t pre_len;
-  int32_t lim;  // positions it sees; 0: none, -1: a row of no request
+  int32_t p0, tokens;  // its rows: places p0 .. p0 + tokens of the order
+  int32_t t0, t1;
+  int32_t tile0, tiles;  // within the list of its kind
+  int32_t wide, shared;
+};
+
+struct AttendTile {
+  int64_t pre_off, tail_off;
+  int32_t pre_len, p0;
+  int32_t row0, rows;  // of the segment's rows
+  int32_t t0, t1;
+  int32_t first;   // the first workgroup (of its head) that takes a piece
+  int32_t pieces;
+  int32_t slot;    // first row of the partial results, `rows` per piece; -1: written out directly
+  int32_t shared;  // its rows have another segment
+};
+
+struct AttendHead {
+  int32_t n_order;    // rows in the order
+  int32_t n_tiles[2];  // wide, narrow
+  int32_t groups[2];   // workgroups per head that take them
+  int64_t units[2];
 };
 
 struct AttendPlanDev {
-  AttendRow* rows;
-  uint32_t* flags;  // per request, PS_R_INVALID
+  AttendHead* head;
+  uint32_t* flags;    // per request: PS_R_INVALID
+  int32_t* table;     // hash slots: request + 1
+  int32_t* least;     // per slot: the least request
+  int32_t* slot_of;   // per request: its slot, -1 for none
+  int32_t* members;   // per request: of the group it leads
+  int32_t* order;     // requests, groups together, by their least member
+  int32_t* base;      // per place of `order`: first of its rows in the row order
+  int32_t* lead;      // per place of `order`: the place of its group's first member, -1 unshared
+  int32_t* row;       // row order: row of the window
+  int32_t* lim;       // positions it sees
+  int32_t* place;     // its request's place in `order`
+  int32_t* todo;      // requests, later segments, with much to write
+  AttendSeg* segs;    // 2 per place: prefix (first members only), own
+  AttendTile* tiles[2];
+  int64_t* begin[2];  // first unit of each tile
+  float* part;        // partial results: [head][slot rows][dim], weights as numerators
+  float2* part_ml;    // their maxima (times scale * log2 e) and sums
+  int32_t table_mask;
+  int32_t tile_cap[2];
+  int32_t slot_rows;  // per head
+  int32_t groups;     // workgroups per head
 };
 
 struct AttendArgs {
@@ -107,7 +164,8 @@ struct AttendArgs {
   BlockRows q, out;
   float* lse;
   float scale;
-  int32_t heads;
+  int32_t heads, ratio;
+  uint32_t bt_mul, bt_shift;  // t / bt = (umulhi(t, bt_mul) + t) >> bt_shift
 };
 
 }  // namespace ps
@@ -116,5 +174,8 @@ hipError_t ps_launch_kv_write(const ps::BlockCache& c, const ps::BlockWin& w, co
                               const ps::BlockRows& v, hipStream_t s);
 hipError_t ps_launch_kv_read(const ps::BlockCache& c, const ps::BlockWin& w, const ps::BlockRows& k,
                              const ps::BlockRows& v, hipStream_t s);
-hipError_t ps_launch_attend_plan(const ps::AttendPlanDev& p, const ps::BlockWin& w, uint32_t* d_flags, hipStream_t s);
+hipError_t ps_launch_attend_plan(const ps::AttendPlanDev& p, const ps::BlockWin& w, int32_t ratio, uint32_t* d_flags,
+                                 hipStream_t s);
 hipError_t ps_launch_attend(const ps::AttendArgs& a, hipStream_t s);
+// Resident workgroups of the attention kernel per CU.
+int32_t ps_attend_per_cu(int32_t dim);

@@ -1,6 +1,7 @@
 // Entry points of the block cache and its attention: argument checks, plan
 // memory and launches.
 
+#include <algorithm>
 #include <cmath>
 #include <new>
 
@@ -15,6 +16,7 @@ struct ps_attend_plan {
   AttendPlanDev dev{};
   bool planned = false;
   BlockWin win{};  // of the last ps_attend_plan_dev
+  int32_t ratio() const { return heads / kv_heads; }
 };
 
 namespace {
@@ -110,9 +112,61 @@ ps_status kv_rows(ps_ctx* c, bool write, const ps_kv_cache* cache, const ps_kv_w
   return PS_OK;
 }
 
+// Every buffer of a plan: the pointer and its bytes.
+template <class F>
+hipError_t each_buffer(ps_attend_plan* p, F f) {
+  AttendPlanDev& d = p->dev;
+  const size_t n = p->max_req, rows = p->max_rows, part = (size_t)d.slot_rows * p->kv_heads;
+  hipError_t e = hipSuccess;
+  auto one = [&](auto*& ptr, size_t count) {
+    if (e == hipSuccess) e = f(ptr, count * sizeof(*ptr));
+  };
+  one(d.head, 1);
+  one(d.flags, n);
+  one(d.table, (size_t)d.table_mask + 1);
+  one(d.least, (size_t)d.table_mask + 1);
+  one(d.slot_of, n);
+  one(d.members, n);
+  one(d.order, n);
+  one(d.base, n);
+  one(d.lead, n);
+  one(d.row, rows);
+  one(d.lim, rows);
+  one(d.place, rows);
+  one(d.todo, 2 * n);
+  one(d.segs, 2 * n);
+  for (int k = 0; k < 2; ++k) {
+    one(d.tiles[k], d.tile_cap[k]);
+    one(d.begin[k], d.tile_cap[k]);
+  }
+  one(d.part, part * p->dim);
+  one(d.part_ml, part);
+  return e;
+}
+
 void release(ps_attend_plan* p) {
-  p->ctx->pool.release(p->dev.rows);
-  p->ctx->pool.release(p->dev.flags);
+  (void)each_buffer(p, [&](auto*& ptr, size_t) {
+    p->ctx->pool.release(ptr);
+    return hipSuccess;
+  });
+}
+
+// Sizes that hold whatever window of at most max_req requests and max_rows rows.
+void size_plan(ps_attend_plan* p, int32_t num_cus) {
+  AttendPlanDev& d = p->dev;
+  const int64_t n = p->max_req, rows = (int64_t)p->max_rows * p->ratio();
+  int32_t slots = 2;
+  while (slots < 2 * n) slots *= 2;
+  d.table_mask = slots - 1;
+  // a wide tile is full but for the last one of each segment, and a row lies in two segments at most
+  d.tile_cap[0] = (int32_t)(2 * n + 2 * rows / kWideRows + 1);
+  d.tile_cap[1] = (int32_t)(2 * n + 1);
+  d.groups = std::max(1, num_cus * ps_attend_per_cu(p->dim) / p->kv_heads);
+  // Of partial results: each row of a shared segment once, in both of its segments;
+  // and the pieces of tiles that are cut, of which there are fewer than twice
+  // as many as workgroups, for each kind.
+  const int64_t shared = std::min(rows, n * std::max(kShareMaxRows, p->ratio()));
+  d.slot_rows = (int32_t)std::min<int64_t>(2 * shared + 2 * (int64_t)d.groups * (kWideRows + kNarrowRows), INT32_MAX);
 }
 
 }  // namespace
@@ -161,8 +215,8 @@ ps_status ps_attend_plan_create(ps_ctx* c, int32_t n_heads, int32_t n_kv_heads, 
   p->bt = block_tokens;
   p->max_req = max_req;
   p->max_rows = max_rows;
-  hipError_t e = c->pool.grow(&p->dev.rows, (size_t)max_rows * sizeof(AttendRow));
-  if (e == hipSuccess) e = c->pool.grow(&p->dev.flags, (size_t)max_req * sizeof(uint32_t));
+  size_plan(p, c->num_cus);
+  const hipError_t e = each_buffer(p, [&](auto*& ptr, size_t bytes) { return c->pool.grow(&ptr, bytes); });
   if (e != hipSuccess) {
     release(p);
     delete p;
@@ -197,7 +251,7 @@ ps_status ps_attend_plan_dev(ps_attend_plan* p, const ps_kv_window* window, uint
                 p->max_req, p->max_rows);
   DeviceScope ds(c->device);
   const BlockWin w = dev_win(*window, p->bt);
-  if (w.n_req > 0 && w.n_rows > 0) HIP_TRY(c, ps_launch_attend_plan(p->dev, w, d_flags, (hipStream_t)hip_stream));
+  if (w.n_req > 0 && w.n_rows > 0) HIP_TRY(c, ps_launch_attend_plan(p->dev, w, p->ratio(), d_flags, (hipStream_t)hip_stream));
   p->win = w;
   p->planned = true;
   return PS_OK;
@@ -224,7 +278,9 @@ ps_status ps_attend_window_dev(ps_attend_plan* p, const ps_kv_cache* cache, cons
   if (p->win.n_pages > cache->n_pages) return fail(c, PS_E_INVAL, "the window names more pages than the cache has");
   if (none) return PS_OK;
   DeviceScope ds(c->device);
-  AttendArgs a{p->dev, p->win, dev_cache(*cache), dev_rows(*q), dev_rows(*out), lse, scale, p->heads};
+  AttendArgs a{p->dev, p->win, dev_cache(*cache), dev_rows(*q), dev_rows(*out), lse, scale, p->heads, p->ratio(), 0, 0};
+  while ((1 << a.bt_shift) < p->bt) ++a.bt_shift;
+  a.bt_mul = (uint32_t)(((uint64_t)((1 << a.bt_shift) - p->bt) << 32) / p->bt + 1);
   HIP_TRY(c, ps_launch_attend(a, (hipStream_t)hip_stream));
   return PS_OK;
 }
