@@ -20,6 +20,8 @@
 // e4m3 values are brought to the 16-bit type with their power of two as they
 // are staged (exact but for fp16's range), so one kernel serves both.
 
+#include <algorithm>
+
 #include "ps_blocks.h"
 
 namespace ps {
@@ -701,66 +703,101 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_kernel(AttendAr
   }
 }
 
-// Joins the partial results of each row and query head, one wave each, and
-// writes the rows that nothing was computed for.
-template <bool kF16>
+// Joins the partial results of the plan's list of rows, a wave for each row and
+// key / value head, and writes the rows that nothing was computed for.  The pieces' maxima and
+// sums are a lane's each, 64 at a time; LG lanes hold a row of results, so 64 / LG
+// pieces are read at once.
+template <bool kF16, int LG>
 __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int32_t at = (int32_t)(id / a.heads), qh = (int32_t)(id % a.heads);
-  if (at >= a.plan.head->n_order) return;
-  const int32_t head = qh / a.ratio, sub = qh - head * a.ratio, i = a.plan.place[at], lead = a.plan.lead[i];
-  int64_t from[2];
-  int32_t n[2] = {0, 0}, step[2] = {0, 0};
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const int32_t si = k == 0 ? 2 * i + 1 : 2 * lead;
-    if (si < 0) continue;
-    const AttendSeg& s = a.plan.segs[si];
-    if (s.tiles == 0) continue;
-    const int32_t x = (at - s.p0) * a.ratio + sub, ti = s.wide ? x / kWideRows : 0;
-    const AttendTile& t = a.plan.tiles[s.wide ? 0 : 1][s.tile0 + ti];
-    if (t.pieces > 0 && t.slot < 0) return;  // written out already
-    n[k] = t.pieces;
-    step[k] = t.rows;
-    from[k] = (int64_t)head * a.plan.slot_rows + t.slot + (x - t.row0);
-  }
-  const int32_t total = n[0] + n[1];
-  auto slot = [&](int32_t j) { return j < n[0] ? from[0] + (int64_t)j * step[0] : from[1] + (int64_t)(j - n[0]) * step[1]; };
-  float top = -INFINITY;
-  for (int32_t j = lane; j < total; j += 64) top = fmaxf(top, a.plan.part_ml[slot(j)].x);
-  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-  const float mc = top == -INFINITY ? 0.0f : top;
-  const int32_t D = a.cache.dim, d = 4 * lane;
-  f32x4 acc = {0, 0, 0, 0};
-  float l = 0;
-  for (int32_t j = 0; j < total; ++j) {
-    const int64_t s = slot(j);
-    const float2 x = a.plan.part_ml[s];
-    const float f = __builtin_amdgcn_exp2f(x.x - mc);
-    l = __builtin_fmaf(x.y, f, l);
-    if (d < D) {
-      const f32x4 o = *(const f32x4*)(a.plan.part + s * D + d);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(o[e], f, acc[e]);
+  const int lane = threadIdx.x & 63, sub = lane / LG, d = 4 * (lane % LG);
+  const int32_t D = a.cache.dim;
+  const int64_t n = (int64_t)a.plan.head->n_joins * a.cache.heads;
+  for (int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); id < n; id += (int64_t)gridDim.x * 4) {
+    const AttendJoin x = a.plan.joins[id / a.cache.heads];
+    const int32_t head = (int32_t)(id % a.cache.heads);
+    const int64_t row = a.plan.row[x.place];
+    if (x.sub < 0) {
+      for (int32_t h = head * a.ratio; h < (head + 1) * a.ratio; ++h) {
+        if (sub == 0 && d < D)
+          *(u32x2*)(a.out.data + 2 * (row * a.out.row + (int64_t)h * a.out.head + d)) = u32x2{0, 0};
+        if (a.lse && lane == 0) a.lse[row * a.heads + h] = -INFINITY;
+      }
+      continue;
     }
+    const bool empty = a.plan.lim[x.place] <= 0;
+    int64_t from[2] = {0, 0};
+    int32_t count[2] = {0, 0}, step[2] = {0, 0};
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      if (x.tile[k] < 0) continue;
+      const AttendTile& t = a.plan.tiles[x.tile[k] & kWideBit ? 0 : 1][x.tile[k] & (kWideBit - 1)];
+      count[k] = t.pieces;
+      step[k] = t.rows;
+      from[k] = (int64_t)head * a.plan.slot_rows + t.slot + ((x.place - t.p0) * a.ratio + x.sub - t.row0);
+    }
+    const int32_t total = count[0] + count[1];
+    auto slot = [&](int32_t j) {
+      const bool own = j < count[0];
+      return (own ? from[0] : from[1]) + (int64_t)(own ? j : j - count[0]) * (own ? step[0] : step[1]);
+    };
+    float2 ml = {-INFINITY, 0.0f};
+    if (lane < total) ml = a.plan.part_ml[slot(lane)];
+    float top = ml.x;
+    for (int32_t j = 64 + lane; j < total; j += 64) top = fmaxf(top, a.plan.part_ml[slot(j)].x);
+    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+    const float mc = top == -INFINITY ? 0.0f : top;
+    f32x4 acc = {0, 0, 0, 0};
+    float l = 0;
+    for (int32_t j0 = 0; j0 < total; j0 += 64) {
+      if (j0 > 0) {
+        ml = float2{-INFINITY, 0.0f};
+        if (j0 + lane < total) ml = a.plan.part_ml[slot(j0 + lane)];
+      }
+      const float f = __builtin_amdgcn_exp2f(ml.x - mc);
+      float part = ml.y * f;
+      for (int o = 32; o > 0; o >>= 1) part += __shfl_xor(part, o, 64);
+      l += part;
+      const int32_t m = min(64, total - j0);
+      constexpr int kAtOnce = 4, kStep = 64 / LG;
+      for (int32_t j = 0; j < m; j += kAtOnce * kStep) {
+        f32x4 o[kAtOnce];
+        float w[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+          const int32_t at = j + u * kStep + sub, in = min(at, m - 1);
+          w[u] = __shfl(f, in, 64);
+          o[u] = f32x4{0, 0, 0, 0};
+          if (at < m && d < D) o[u] = *(const f32x4*)(a.plan.part + slot(j0 + in) * D + d);
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            acc[e] = j + u * kStep + sub < m ? __builtin_fmaf(o[u][e], w[u], acc[e]) : acc[e];
+      }
+    }
+#pragma unroll
+    for (int o = LG; o < 64; o <<= 1)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], o, 64);
+    const int32_t h = head * a.ratio + x.sub;
+    const float inv = 1.0f / l;
+    if (sub == 0 && d < D) {
+      u32x2 w = {0, 0};
+      if (!empty) w = u32x2{pack<kF16>(acc[0] * inv, acc[1] * inv), pack<kF16>(acc[2] * inv, acc[3] * inv)};
+      *(u32x2*)(a.out.data + 2 * (row * a.out.row + (int64_t)h * a.out.head + d)) = w;
+    }
+    if (a.lse && lane == 0) a.lse[row * a.heads + h] = empty ? -INFINITY : __builtin_fmaf(top, kLn2, __logf(l));
   }
-  const bool empty = a.plan.lim[at] <= 0;
-  const float inv = 1.0f / l;
-  const int64_t row = a.plan.row[at];
-  if (d < D) {
-    u32x2 x = {0, 0};
-    if (!empty) x = u32x2{pack<kF16>(acc[0] * inv, acc[1] * inv), pack<kF16>(acc[2] * inv, acc[3] * inv)};
-    *(u32x2*)(a.out.data + 2 * (row * a.out.row + (int64_t)qh * a.out.head + d)) = x;
-  }
-  if (a.lse && lane == 0) a.lse[row * a.heads + qh] = empty ? -INFINITY : __builtin_fmaf(top, kLn2, __logf(l));
 }
 
-template <bool kF16, bool kQ8>
-void launch(const AttendArgs& a, dim3 grid, hipStream_t s) {
-  if (a.cache.dim <= 64) hipLaunchKernelGGL((attend_kernel<kF16, kQ8, 64>), grid, dim3(256), 0, s, a);
-  else if (a.cache.dim <= 128) hipLaunchKernelGGL((attend_kernel<kF16, kQ8, 128>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((attend_kernel<kF16, kQ8, 256>), grid, dim3(256), 0, s, a);
+template <bool kF16, bool kQ8, int DP>
+void launch(const AttendArgs& a, int32_t num_cus, hipStream_t s) {
+  const dim3 grid((unsigned)(a.plan.groups * a.cache.heads));
+  const int64_t rows = (int64_t)a.win.n_rows * a.heads;
+  const dim3 join((unsigned)std::min<int64_t>((rows + 3) / 4, 8 * num_cus));
+  hipLaunchKernelGGL((attend_kernel<kF16, kQ8, DP>), grid, dim3(256), 0, s, a);
+  hipLaunchKernelGGL((join_kernel<kF16, DP / 4>), join, dim3(256), 0, s, a);
 }
 
 }  // namespace
@@ -769,15 +806,18 @@ void launch(const AttendArgs& a, dim3 grid, hipStream_t s) {
 
 int32_t ps_attend_per_cu(int32_t dim) { return dim <= 128 ? 2 : 1; }
 
-hipError_t ps_launch_attend(const ps::AttendArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)(a.plan.groups * a.cache.heads));
-  const dim3 join((unsigned)(((int64_t)a.win.n_rows * a.heads + 3) / 4));
+hipError_t ps_launch_attend(const ps::AttendArgs& a, int32_t num_cus, hipStream_t s) {
   const bool f16 = a.q.dtype == PS_T_F16, quant = a.cache.dtype == PS_T_E4M3;
-  if (f16 && quant) ps::launch<true, true>(a, grid, s);
-  else if (f16) ps::launch<true, false>(a, grid, s);
-  else if (quant) ps::launch<false, true>(a, grid, s);
-  else ps::launch<false, false>(a, grid, s);
-  if (f16) hipLaunchKernelGGL(ps::join_kernel<true>, join, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(ps::join_kernel<false>, join, dim3(256), 0, s, a);
+#define PS_DIM(F, Q)                                                       \
+  do {                                                                     \
+    if (a.cache.dim <= 64) ps::launch<F, Q, 64>(a, num_cus, s);            \
+    else if (a.cache.dim <= 128) ps::launch<F, Q, 128>(a, num_cus, s);     \
+    else ps::launch<F, Q, 256>(a, num_cus, s);                             \
+  } while (0)
+  if (f16 && quant) PS_DIM(true, true);
+  else if (f16) PS_DIM(true, false);
+  else if (quant) PS_DIM(false, true);
+  else PS_DIM(false, false);
+#undef PS_DIM
   return hipGetLastError();
 }

@@ -157,7 +157,7 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
       }
     }
   __syncthreads();
-  const int64_t n_order = scan_all(
+  scan_all(
       n, sums, [&](int32_t i) { return (int64_t)(w.row_off[(keys[i] & 8191u) + 1] - w.row_off[keys[i] & 8191u]); },
       [&](int32_t i, int64_t at) { p.base[i] = (int32_t)at; });
   __syncthreads();
@@ -240,7 +240,7 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
           if (p.segs[k].wide == (kind == 0)) p.segs[k].tile0 = (int32_t)at;
         });
   __syncthreads();
-  auto write_tile = [&](const AttendSeg& s, int32_t k) {
+  auto write_tile = [&](const AttendSeg& s, int32_t k, int32_t prefix) {
     AttendTile t{};
     t.pre_off = s.pre_off;
     t.tail_off = s.tail_off;
@@ -252,26 +252,26 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
     // (a request's later rows see more: none of the tile's sees more than its last)
     t.t1 = min(s.t1, p.lim[s.p0 + (t.row0 + t.rows - 1) / ratio]);
     t.shared = s.shared;
+    t.prefix = prefix;
     p.tiles[s.wide ? 0 : 1][s.tile0 + k] = t;
   };
   for (int32_t k = tid; k < 2 * n; k += kThreads) {
     const AttendSeg s = p.segs[k];
     if (s.tiles <= 4)
-      for (int32_t j = 0; j < s.tiles; ++j) write_tile(s, j);
+      for (int32_t j = 0; j < s.tiles; ++j) write_tile(s, j, !(k & 1));
     else
       p.todo[atomicAdd(&n_todo, 1)] = k;
   }
   __syncthreads();
   for (int32_t k = wave; k < n_todo; k += kWaves) {
     const AttendSeg s = p.segs[p.todo[k]];
-    for (int32_t j = lane; j < s.tiles; j += 64) write_tile(s, j);
+    for (int32_t j = lane; j < s.tiles; j += 64) write_tile(s, j, !(p.todo[k] & 1));
   }
   __syncthreads();
 
   // Units end to end, who takes them, and the rows of partial results.
   int64_t slots = 0;
   AttendHead h{};
-  h.n_order = (int32_t)n_order;
   for (int kind = 0; kind < 2; ++kind) {
     AttendTile* tiles = p.tiles[kind];
     auto units_of = [&](int32_t k) { return (int64_t)((max(0, tiles[k].t1 - tiles[k].t0) + kUnit - 1) / kUnit); };
@@ -301,6 +301,45 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
         });
     __syncthreads();
   }
+
+  // What is to be joined: the rows of own tiles that are kept, with their prefix
+  // tiles; of shared segments that end with the prefix, the rows with the prefix
+  // alone; of everything else that has no pieces, places of empty rows.
+  if (tid == 0) n_todo = 0;
+  __syncthreads();
+  auto push = [&](int32_t place, int32_t sub, int32_t own) {
+    AttendJoin x{place, sub, {own, -1}};
+    const int32_t lead = sub < 0 ? -1 : p.lead[p.place[place]];
+    if (lead >= 0) {
+      const AttendSeg& s = p.segs[2 * lead];
+      x.tile[1] = s.wide ? (s.tile0 + ((place - s.p0) * ratio + sub) / kWideRows) | kWideBit : s.tile0;
+    }
+    p.joins[atomicAdd(&n_todo, 1)] = x;
+  };
+  for (int kind = 0; kind < 2; ++kind) {
+    // a wave per wide tile, a quarter of one per narrow tile
+    const int per = kind == 0 ? 64 : 16;
+    for (int32_t k = tid / per; k < n_tiles[kind]; k += kThreads / per) {
+      const AttendTile t = p.tiles[kind][k];
+      if (t.prefix || (t.pieces > 0 && t.slot < 0)) continue;
+      for (int32_t r = tid % per; r < t.rows; r += per) {
+        const int32_t x = t.row0 + r, at = x / ratio, sub = x - at * ratio;
+        if (t.pieces > 0) push(t.p0 + at, sub, kind == 0 ? k | kWideBit : k);
+        else if (sub == 0 || r == 0) push(t.p0 + at, -1, -1);
+      }
+    }
+  }
+  for (int32_t i = wave; i < n; i += kWaves) {
+    const AttendSeg& s = p.segs[2 * i + 1];
+    if (s.tiles > 0) continue;
+    for (int32_t j = lane; j < s.tokens; j += 64)
+      if (s.shared)
+        for (int32_t sub = 0; sub < ratio; ++sub) push(s.p0 + j, sub, -1);
+      else
+        push(s.p0 + j, -1, -1);
+  }
+  __syncthreads();
+  h.n_joins = n_todo;
   if (tid == 0) *p.head = h;
 }
 

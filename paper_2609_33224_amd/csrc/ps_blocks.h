@@ -123,10 +123,21 @@ struct AttendTile {
   int32_t pieces;
   int32_t slot;    // first row of the partial results, `rows` per piece; -1: written out directly
   int32_t shared;  // its rows have another segment
+  int32_t prefix;  // it is a shared prefix's
+  int32_t pad;
 };
 
+// What the second kernel joins: one row of a tile, or all rows of a place that
+// nothing was computed for.
+struct alignas(16) AttendJoin {
+  int32_t place;    // in the row order
+  int32_t sub;      // query head of the group; -1: all of them, empty
+  int32_t tile[2];  // own, prefix: place in the list of its kind | kWideBit; -1: none
+};
+constexpr int32_t kWideBit = 1 << 30;
+
 struct AttendHead {
-  int32_t n_order;    // rows in the order
+  int32_t n_joins;
   int32_t n_tiles[2];  // wide, narrow
   int32_t groups[2];   // workgroups per head that take them
   int64_t units[2];
@@ -149,6 +160,7 @@ struct AttendPlanDev {
   AttendSeg* segs;    // 2 per place: prefix (first members only), own
   AttendTile* tiles[2];
   int64_t* begin[2];  // first unit of each tile
+  AttendJoin* joins;
   float* part;        // partial results: [head][slot rows][dim], weights as numerators
   float2* part_ml;    // their maxima (times scale * log2 e) and sums
   int32_t table_mask;
@@ -176,6 +188,6 @@ hipError_t ps_launch_kv_read(const ps::BlockCache& c, const ps::BlockWin& w, con
                              const ps::BlockRows& v, hipStream_t s);
 hipError_t ps_launch_attend_plan(const ps::AttendPlanDev& p, const ps::BlockWin& w, int32_t ratio, uint32_t* d_flags,
                                  hipStream_t s);
-hipError_t ps_launch_attend(const ps::AttendArgs& a, hipStream_t s);
+hipError_t ps_launch_attend(const ps::AttendArgs& a, int32_t num_cus, hipStream_t s);
 // Resident workgroups of the attention kernel per CU.
 int32_t ps_attend_per_cu(int32_t dim);

@@ -139,6 +139,8 @@ hipError_t each_buffer(ps_attend_plan* p, F f) {
     one(d.tiles[k], d.tile_cap[k]);
     one(d.begin[k], d.tile_cap[k]);
   }
+  // (a row with partial results each, or a place of empty rows: twice where two tiles have some)
+  one(d.joins, (size_t)d.slot_rows + rows + d.tile_cap[0]);
   one(d.part, part * p->dim);
   one(d.part_ml, part);
   return e;
@@ -281,7 +283,7 @@ ps_status ps_attend_window_dev(ps_attend_plan* p, const ps_kv_cache* cache, cons
   AttendArgs a{p->dev, p->win, dev_cache(*cache), dev_rows(*q), dev_rows(*out), lse, scale, p->heads, p->ratio(), 0, 0};
   while ((1 << a.bt_shift) < p->bt) ++a.bt_shift;
   a.bt_mul = (uint32_t)(((uint64_t)((1 << a.bt_shift) - p->bt) << 32) / p->bt + 1);
-  HIP_TRY(c, ps_launch_attend(a, (hipStream_t)hip_stream));
+  HIP_TRY(c, ps_launch_attend(a, c->num_cus, (hipStream_t)hip_stream));
   return PS_OK;
 }
 
