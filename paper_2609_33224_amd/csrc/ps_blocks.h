@@ -183,9 +183,9 @@ struct AttendArgs {
 }  // namespace ps
 
 hipError_t ps_launch_kv_write(const ps::BlockCache& c, const ps::BlockWin& w, const ps::BlockRows& k,
-                              const ps::BlockRows& v, hipStream_t s);
+                              const ps::BlockRows& v, int32_t num_cus, hipStream_t s);
 hipError_t ps_launch_kv_read(const ps::BlockCache& c, const ps::BlockWin& w, const ps::BlockRows& k,
-                             const ps::BlockRows& v, hipStream_t s);
+                             const ps::BlockRows& v, int32_t num_cus, hipStream_t s);
 hipError_t ps_launch_attend_plan(const ps::AttendPlanDev& p, const ps::BlockWin& w, int32_t ratio, uint32_t* d_flags,
                                  hipStream_t s);
 hipError_t ps_launch_attend(const ps::AttendArgs& a, int32_t num_cus, hipStream_t s);

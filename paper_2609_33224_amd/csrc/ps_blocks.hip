@@ -108,7 +108,7 @@ ps_status kv_rows(ps_ctx* c, bool write, const ps_kv_cache* cache, const ps_kv_w
   DeviceScope ds(c->device);
   const BlockWin dw = dev_win(*w, cache->block_tokens);
   HIP_TRY(c, (write ? ps_launch_kv_write : ps_launch_kv_read)(dev_cache(*cache), dw, dev_rows(*k), dev_rows(*v),
-                                                              (hipStream_t)stream));
+                                                              c->num_cus, (hipStream_t)stream));
   return PS_OK;
 }
 

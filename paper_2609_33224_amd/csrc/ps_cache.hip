@@ -6,6 +6,8 @@
 // store is one contiguous run per row and head: 2 D bytes in, D (or 2 D) out.
 // Both passes are bound by that traffic, and by launch latency for a few rows.
 
+#include <algorithm>
+
 #include "ps_blocks.h"
 
 namespace ps {
@@ -30,23 +32,60 @@ __device__ inline float element(const u32x4& x, int j) {
   return __builtin_bit_cast(float, j & 1 ? w & 0xFFFF0000u : w << 16);
 }
 
-// Units of work: (row, K or V, head), the head fastest, LP lanes each.
-struct Unit {
-  int32_t row, head;
-  int which;  // 0: K, 1: V
-  int32_t d;  // first element of the lane
+// A wave takes `per` rows (kMaxPer at most): a lane each finds where they lie, and the
+// wave then moves their units (a head's K or V of a row, LP lanes), kAtOnce
+// steps of 64 lanes at a time, so that the lookups' latency is paid once per wave and several
+// loads are in flight.
+constexpr int kMaxPer = 8;
+constexpr int kAtOnce = 4;
+
+struct Place {
+  int64_t page;
+  int32_t slot;
+  int32_t state;  // 0: no request's, 1: without a place, 2: in the page
 };
+
+struct Unit {
+  int64_t at, xat;  // in the cache: first element of the lane, exponent of the row
+  int64_t row;
+  int32_t head, d, state;
+  bool v;
+};
+
+// The lane's unit of step `step`; state 0 where there is none.
 template <int LP>
-__device__ inline bool unit_of(const BlockWin& w, int32_t heads, Unit* u) {
-  const int64_t id = ((int64_t)blockIdx.x * kBlock + threadIdx.x) / LP;
-  const int64_t per_row = 2 * heads;
-  const int64_t row = id / per_row;
-  const int32_t rest = (int32_t)(id - row * per_row);
-  u->row = (int32_t)row;
-  u->which = rest >= heads;
-  u->head = rest - u->which * heads;
-  u->d = (threadIdx.x % LP) * 8;
-  return row < w.n_rows;
+__device__ inline Unit unit_of(const BlockCache& c, const Place& mine, int32_t row0, int32_t per, int32_t step) {
+  const int lane = threadIdx.x & 63;
+  const int32_t id = (step * 64 + lane) / LP, row = id / (2 * c.heads), rest = id - row * 2 * c.heads;
+  const int from = row < per ? row : 0;
+  Unit u;
+  u.state = __shfl(mine.state, from, 64);
+  const int64_t page = __shfl((long long)mine.page, from, 64);
+  const int32_t slot = __shfl(mine.slot, from, 64);
+  u.v = rest >= c.heads;
+  u.head = rest - (u.v ? c.heads : 0);
+  u.row = row0 + row;
+  u.d = (lane % LP) * 8;
+  const int32_t r = u.head * c.bt + slot;
+  u.at = page * c.page_stride + (int64_t)r * c.dim + u.d;
+  u.xat = page * c.exp_stride + r;
+  if (row >= per) u.state = 0;
+  return u;
+}
+
+__device__ inline Place place_of(const BlockWin& w, int32_t row0, int32_t per) {
+  const int lane = threadIdx.x & 63;
+  Place p{0, 0, 0};
+  if (lane < per && row0 + lane < w.n_rows) {
+    bool has;
+    const bool in = block_locate(w, row0 + lane, &has, &p.page, &p.slot);
+    p.state = in ? 2 : has ? 1 : 0;
+    if (!in) {
+      p.page = 0;
+      p.slot = 0;
+    }
+  }
+  return p;
 }
 
 // An e4m3 code is x / 2^e rounded once (to nearest, ties to even), with e the
@@ -55,94 +94,124 @@ __device__ inline bool unit_of(const BlockWin& w, int32_t heads, Unit* u) {
 // product of 4 significant bits with a power of two.  The exponent comes from
 // the bits of that magnitude: 448 = 1.75 * 2^8.
 template <int LP, bool kF16, bool kQuant>
-__global__ __launch_bounds__(kBlock) void write_kernel(BlockCache c, BlockWin w, BlockRows k, BlockRows v) {
-  Unit u;
-  if (!unit_of<LP>(w, c.heads, &u)) return;
-  bool has;
-  int64_t page;
-  int32_t slot;
-  if (!block_locate(w, u.row, &has, &page, &slot)) return;  // (the same for all lanes of the unit)
-  const BlockRows& src = u.which ? v : k;
-  u32x4 x = {0, 0, 0, 0};
-  const bool in = u.d < c.dim;
-  if (in) x = *(const u32x4*)(src.data + 2 * (u.row * src.row + u.head * src.head + u.d));
-  const int64_t at = page * c.page_stride + ((int64_t)u.head * c.bt + slot) * c.dim + u.d;
-  unsigned char* dst = u.which ? c.v : c.k;
-  if (!kQuant) {
-    if (in) *(u32x4*)(dst + 2 * at) = x;
-    return;
-  }
-  float f[8];
-  uint32_t big = 0;
+__global__ __launch_bounds__(kBlock) void write_kernel(BlockCache c, BlockWin w, BlockRows k, BlockRows v, int32_t per) {
+  const int64_t first = ((int64_t)blockIdx.x * (kBlock / 64) + (threadIdx.x >> 6)) * per;
+  if (first >= w.n_rows) return;
+  const int32_t row0 = (int32_t)first, steps = (per * 2 * c.heads * LP + 63) / 64;
+  const Place mine = place_of(w, row0, per);
+  for (int32_t s0 = 0; s0 < steps; s0 += kAtOnce) {
+    Unit u[kAtOnce];
+    u32x4 x[kAtOnce];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    f[j] = element<kF16>(x, j);
-    const uint32_t a = __builtin_bit_cast(uint32_t, f[j]) & 0x7FFFFFFFu;
-    big = max(big, a < 0x7F800000u ? a : 0u);
-  }
+    for (int i = 0; i < kAtOnce; ++i) {
+      u[i] = unit_of<LP>(c, mine, row0, per, s0 + i);
+      x[i] = u32x4{0, 0, 0, 0};
+      const BlockRows& src = u[i].v ? v : k;
+      if (u[i].state == 2 && u[i].d < c.dim)
+        x[i] = *(const u32x4*)(src.data + 2 * (u[i].row * src.row + u[i].head * src.head + u[i].d));
+    }
 #pragma unroll
-  for (int o = LP / 2; o > 0; o >>= 1) big = max(big, (uint32_t)__shfl_xor((int)big, o, 64));
-  const int e = max((int)(big >> 23) - 127 - 8 + ((big & 0x7FFFFFu) > 0x600000u ? 1 : 0), -126);
-  const float s = __builtin_bit_cast(float, (uint32_t)(127 - e) << 23);
+    for (int i = 0; i < kAtOnce; ++i) {
+      const bool put = u[i].state == 2 && u[i].d < c.dim;
+      unsigned char* dst = u[i].v ? c.v : c.k;
+      if (!kQuant) {
+        if (put) *(u32x4*)(dst + 2 * u[i].at) = x[i];
+        continue;
+      }
+      float f[8];
+      uint32_t big = 0;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float y = f[j] * s;
-    f[j] = y > 448.0f ? 448.0f : y < -448.0f ? -448.0f : y;  // (infinities; NaN stays)
-  }
-  u32x2 o;
+      for (int j = 0; j < 8; ++j) {
+        f[j] = element<kF16>(x[i], j);
+        const uint32_t a = __builtin_bit_cast(uint32_t, f[j]) & 0x7FFFFFFFu;
+        big = max(big, a < 0x7F800000u ? a : 0u);
+      }
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    int p = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * h], f[4 * h + 1], 0, false);
-    o[h] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f[4 * h + 2], f[4 * h + 3], p, true);
-  }
-  if (in) *(u32x2*)(dst + at) = o;
-  if (u.d == 0) (u.which ? c.vx : c.kx)[page * c.exp_stride + (int64_t)u.head * c.bt + slot] = (uint8_t)(e + 127);
-}
-
-template <int LP, bool kF16, bool kQuant>
-__global__ __launch_bounds__(kBlock) void read_kernel(BlockCache c, BlockWin w, BlockRows k, BlockRows v) {
-  Unit u;
-  if (!unit_of<LP>(w, c.heads, &u)) return;
-  if (u.d >= c.dim) return;
-  bool has;
-  int64_t page;
-  int32_t slot;
-  u32x4 x = {0, 0, 0, 0};
-  if (block_locate(w, u.row, &has, &page, &slot)) {
-    const int64_t at = page * c.page_stride + ((int64_t)u.head * c.bt + slot) * c.dim + u.d;
-    const unsigned char* src = u.which ? c.v : c.k;
-    if (!kQuant) {
-      x = *(const u32x4*)(src + 2 * at);
-    } else {
-      const u32x2 p = *(const u32x2*)(src + at);
-      const uint32_t ex = (u.which ? c.vx : c.kx)[page * c.exp_stride + (int64_t)u.head * c.bt + slot];
-      const float s = __builtin_bit_cast(float, ex << 23);
+      for (int o = LP / 2; o > 0; o >>= 1) big = max(big, (uint32_t)__shfl_xor((int)big, o, 64));
+      const int e = max((int)(big >> 23) - 127 - 8 + ((big & 0x7FFFFFu) > 0x600000u ? 1 : 0), -126);
+      const float s = __builtin_bit_cast(float, (uint32_t)(127 - e) << 23);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float y = f[j] * s;
+        f[j] = y > 448.0f ? 448.0f : y < -448.0f ? -448.0f : y;  // (infinities; NaN stays)
+      }
+      u32x2 o;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        if (kF16) {
-          x[2 * h] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)p[h], s, false));
-          x[2 * h + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)p[h], s, true));
-        } else {
-          x[2 * h] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)p[h], s, false));
-          x[2 * h + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)p[h], s, true));
-        }
+        const int p = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * h], f[4 * h + 1], 0, false);
+        o[h] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f[4 * h + 2], f[4 * h + 3], p, true);
+      }
+      if (put) {
+        *(u32x2*)(dst + u[i].at) = o;
+        if (u[i].d == 0) (u[i].v ? c.vx : c.kx)[u[i].xat] = (uint8_t)(e + 127);
       }
     }
   }
-  const BlockRows& dst = u.which ? v : k;
-  if (has) *(u32x4*)(dst.data + 2 * (u.row * dst.row + u.head * dst.head + u.d)) = x;
+}
+
+template <int LP, bool kF16, bool kQuant>
+__global__ __launch_bounds__(kBlock) void read_kernel(BlockCache c, BlockWin w, BlockRows k, BlockRows v, int32_t per) {
+  const int64_t first = ((int64_t)blockIdx.x * (kBlock / 64) + (threadIdx.x >> 6)) * per;
+  if (first >= w.n_rows) return;
+  const int32_t row0 = (int32_t)first, steps = (per * 2 * c.heads * LP + 63) / 64;
+  const Place mine = place_of(w, row0, per);
+  for (int32_t s0 = 0; s0 < steps; s0 += kAtOnce) {
+    Unit u[kAtOnce];
+    u32x4 x[kAtOnce];
+    uint32_t ex[kAtOnce];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      u[i] = unit_of<LP>(c, mine, row0, per, s0 + i);
+      x[i] = u32x4{0, 0, 0, 0};
+      ex[i] = 127;
+      if (u[i].state == 2 && u[i].d < c.dim) {
+        const unsigned char* src = u[i].v ? c.v : c.k;
+        if (kQuant) {
+          const u32x2 y = *(const u32x2*)(src + u[i].at);
+          x[i][0] = y[0];
+          x[i][1] = y[1];
+          ex[i] = (u[i].v ? c.vx : c.kx)[u[i].xat];
+        } else {
+          x[i] = *(const u32x4*)(src + 2 * u[i].at);
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      u32x4 o = x[i];
+      if (kQuant) {
+        const float s = __builtin_bit_cast(float, ex[i] << 23);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int p = (int)x[i][h];
+          if (kF16) {
+            o[2 * h] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(p, s, false));
+            o[2 * h + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(p, s, true));
+          } else {
+            o[2 * h] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(p, s, false));
+            o[2 * h + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(p, s, true));
+          }
+        }
+      }
+      const BlockRows& dst = u[i].v ? v : k;
+      if (u[i].state > 0 && u[i].d < c.dim)
+        *(u32x4*)(dst.data + 2 * (u[i].row * dst.row + u[i].head * dst.head + u[i].d)) = o;
+    }
+  }
 }
 
 template <int LP>
 hipError_t launch(bool write, const BlockCache& c, const BlockWin& w, const BlockRows& k, const BlockRows& v,
-                  hipStream_t s) {
-  const int64_t lanes = (int64_t)w.n_rows * 2 * c.heads * LP;
-  const dim3 grid((unsigned)((lanes + kBlock - 1) / kBlock)), block(kBlock);
+                  int32_t num_cus, hipStream_t s) {
+  // one row a wave until every CU has 16 waves, then more: their lookups go side by side
+  const int32_t per = (int32_t)std::min<int64_t>(kMaxPer, std::max<int64_t>(1, w.n_rows / (16 * num_cus)));
+  const int64_t waves = ((int64_t)w.n_rows + per - 1) / per;
+  const dim3 grid((unsigned)((waves + kBlock / 64 - 1) / (kBlock / 64))), block(kBlock);
   const bool f16 = k.dtype == PS_T_F16, quant = c.dtype == PS_T_E4M3;
-#define PS_ROWS(F, Q)                                                                    \
-  do {                                                                                   \
-    if (write) hipLaunchKernelGGL((write_kernel<LP, F, Q>), grid, block, 0, s, c, w, k, v); \
-    else hipLaunchKernelGGL((read_kernel<LP, F, Q>), grid, block, 0, s, c, w, k, v);        \
+#define PS_ROWS(F, Q)                                                                            \
+  do {                                                                                           \
+    if (write) hipLaunchKernelGGL((write_kernel<LP, F, Q>), grid, block, 0, s, c, w, k, v, per); \
+    else hipLaunchKernelGGL((read_kernel<LP, F, Q>), grid, block, 0, s, c, w, k, v, per);        \
   } while (0)
   if (!quant) PS_ROWS(false, false);  // moved as they are
   else if (f16) PS_ROWS(true, true);
@@ -152,11 +221,11 @@ hipError_t launch(bool write, const BlockCache& c, const BlockWin& w, const Bloc
 }
 
 hipError_t rows(bool write, const BlockCache& c, const BlockWin& w, const BlockRows& k, const BlockRows& v,
-                hipStream_t s) {
-  if (c.dim <= 32) return launch<4>(write, c, w, k, v, s);
-  if (c.dim <= 64) return launch<8>(write, c, w, k, v, s);
-  if (c.dim <= 128) return launch<16>(write, c, w, k, v, s);
-  return launch<32>(write, c, w, k, v, s);
+                int32_t num_cus, hipStream_t s) {
+  if (c.dim <= 32) return launch<4>(write, c, w, k, v, num_cus, s);
+  if (c.dim <= 64) return launch<8>(write, c, w, k, v, num_cus, s);
+  if (c.dim <= 128) return launch<16>(write, c, w, k, v, num_cus, s);
+  return launch<32>(write, c, w, k, v, num_cus, s);
 }
 
 }  // namespace
@@ -164,11 +233,11 @@ hipError_t rows(bool write, const BlockCache& c, const BlockWin& w, const BlockR
 }  // namespace ps
 
 hipError_t ps_launch_kv_write(const ps::BlockCache& c, const ps::BlockWin& w, const ps::BlockRows& k,
-                              const ps::BlockRows& v, hipStream_t s) {
-  return ps::rows(true, c, w, k, v, s);
+                              const ps::BlockRows& v, int32_t num_cus, hipStream_t s) {
+  return ps::rows(true, c, w, k, v, num_cus, s);
 }
 
 hipError_t ps_launch_kv_read(const ps::BlockCache& c, const ps::BlockWin& w, const ps::BlockRows& k,
-                             const ps::BlockRows& v, hipStream_t s) {
-  return ps::rows(false, c, w, k, v, s);
+                             const ps::BlockRows& v, int32_t num_cus, hipStream_t s) {
+  return ps::rows(false, c, w, k, v, num_cus, s);
 }
