@@ -8,12 +8,12 @@
 // in the place where the second product takes them: the k index of a matrix
 // product may be permuted, and is, so that it names the positions that the lane holds.
 //
-// A workgroup takes an equal run of the units of its head's tiles (AttendPlanDev).
+// A workgroup takes an equal run of the units of its head's wide tiles (AttendPlanDev),
+// then each of its waves one of the narrow tiles.
 //  - A narrow tile (16 rows at most: the rows of one request that decodes) is
-//    bound by the bytes of its keys and values.  Each wave takes
-//    32 positions of its own in turn, keys straight from memory into the matrix
-//    operand, values through a wave's part of shared memory, where the
-//    transposing read turns them; the four waves' results are joined at the end.
+//    bound by the bytes of its keys and values, so each wave takes a run of its
+//    own: keys straight from memory into the matrix operand, values through the
+//    wave's part of shared memory, where the transposing read turns them.
 //  - A wide tile (128 rows: a prefix that many requests share, a prompt) is
 //    bound by the matrix cores: 64 positions are staged in shared memory for the four
 //    waves, which have 32 rows each.
@@ -234,15 +234,19 @@ __device__ inline int vswz(int row, int chunk) {
   return row * (DP * 2) + ((chunk ^ ((row & 7) << 1)) & (DP / 8 - 1)) * 16;
 }
 
+// Positions of a narrow step: enough that a wave has 16 KB of a head of 128 in flight.
+constexpr int narrow_positions(bool kQ8, int DP) { return kQ8 && DP <= 128 ? 64 : 32; }
+
 template <bool kF16, bool kQ8, int DP, int RB>
-__device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char* smem, float2* ml) {
+__device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char* vs) {
+  constexpr int kTok = narrow_positions(kQ8, DP);
+  constexpr int kH = kTok / 16;                       // rows of positions in the first product
+  constexpr int kX = kTok / 32;                       // steps of the second product
   constexpr int kSteps = DP / 32;                     // of the first product
   constexpr int kLoads = kQ8 ? DP / 64 : DP / 32;     // 16-byte loads per lane and 16 positions
   constexpr int kDB = DP / 16;                        // blocks of the second product
-  const int lane = fresh(threadIdx.x & 63), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int col = lane & 15, g = lane >> 4;
+  const int lane = fresh(threadIdx.x & 63), col = lane & 15, g = lane >> 4;
   const int D = a.cache.dim;
-  unsigned char* vs = smem + wave * 32 * DP * 2;
 
   u32x4 q[RB][kSteps];
   int32_t lim[RB], least = INT32_MAX;
@@ -268,16 +272,16 @@ __device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char*
   }
 
   const int32_t last = p.tb - 1;
-  uint32_t page[2];
-  u32x4 kr[2][kLoads], vr[2][kLoads];
-  uint32_t kx[2], vx[2];
+  uint32_t page[kH];
+  u32x4 kr[kH][kLoads], vr[kH][kLoads];
+  uint32_t kx[kH], vx[kH];
   auto pages = [&](int32_t t) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) page[h] = page_of(a, p.chain, min(t + 16 * h + col, last));
+    for (int h = 0; h < kH; ++h) page[h] = page_of(a, p.chain, min(t + 16 * h + col, last));
   };
   auto loads = [&](int32_t t) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < kH; ++h) {
       const Spot s = spot_of(a, p.head, page[h], min(t + 16 * h + col, last));
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
@@ -295,20 +299,17 @@ __device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char*
     }
   };
 
-  int32_t t = p.ta + 32 * wave;
-  if (t < p.tb) {
-    pages(t);
-    loads(t);
-    pages(t + 128);
-  }
-  for (; t < p.tb; t += 128) {
-    // Values into shared memory.  Where a row may not see all of the 32, their
+  pages(p.ta);
+  loads(p.ta);
+  pages(p.ta + kTok);
+  for (int32_t t = p.ta; t < p.tb; t += kTok) {
+    // Values into shared memory.  Where a row may not see all of the step's, their
     // infinities and NaN are taken out, since a weight of 0 would not take them
     // away; the rows that see them get them below.
-    const bool masked = t + 32 > p.tb || t + 32 > least;  // (the same for the wave)
+    const bool masked = t + kTok > p.tb || t + kTok > least;  // (the same for the wave)
     uint32_t odd = 0;
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < kH; ++h)
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
         const int row = 16 * h + col;
@@ -326,10 +327,10 @@ __device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char*
           *(u32x4*)(vs + vswz<DP>(row, 4 * i + g)) = vr[h][i];
         }
       }
-    // scores: position 16 h + 4 g + i of the 32, row b * 16 + col
-    f32x4 s[RB][2];
+    // scores: position 16 h + 4 g + i of the step, row b * 16 + col
+    f32x4 s[RB][kH];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < kH; ++h) {
 #pragma unroll
       for (int b = 0; b < RB; ++b) s[b][h] = f32x4{0, 0, 0, 0};
 #pragma unroll
@@ -345,54 +346,58 @@ __device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char*
         for (int b = 0; b < RB; ++b) s[b][h] = mfma16<kF16>(ka, q[b][st], s[b][h]);
       }
     }
-    if (t + 128 < p.tb) {
-      loads(t + 128);
-      pages(t + 256);
+    if (t + kTok < p.tb) {
+      loads(t + kTok);
+      pages(t + 2 * kTok);
     }
+    // (the rows that other lanes wrote)
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 
     if (masked) {
 #pragma unroll
       for (int b = 0; b < RB; ++b)
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < kH; ++h)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             if (t + 16 * h + 4 * g + i >= min(lim[b], p.tb)) s[b][h][i] = -INFINITY;
     }
-    u32x4 pr[RB];
+    u32x4 pr[RB][kX];
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
       float top = s[b][0][0];
 #pragma unroll
-      for (int i = 1; i < 8; ++i) top = fmaxf(top, s[b][i >> 2][i & 3]);
+      for (int i = 1; i < 4 * kH; ++i) top = fmaxf(top, s[b][i >> 2][i & 3]);
       top = fmaxf(top, __shfl_xor(top, 16, 64));
       top = fmaxf(top, __shfl_xor(top, 32, 64));
       const float nm = fmaxf(m[b], top), mc = nm == -INFINITY ? 0.0f : nm * p.c;
       const float f = __builtin_amdgcn_exp2f(__builtin_fmaf(m[b], p.c, -mc));
       m[b] = nm;
-      float e[8], sum = 0;
+      float sum = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i >> 2][i & 3], p.c, -mc));
-        sum += e[i];
-      }
+      for (int x = 0; x < kX; ++x)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const f32x4& v = s[b][2 * x + (i >> 1)];
+          const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(v[(2 * i) & 3], p.c, -mc));
+          const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(v[(2 * i + 1) & 3], p.c, -mc));
+          sum += e0 + e1;
+          pr[b][x][i] = pack<kF16>(e0, e1);
+        }
       l[b] = __builtin_fmaf(l[b], f, sum);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) pr[b][i] = pack<kF16>(e[2 * i], e[2 * i + 1]);
 #pragma unroll
       for (int k = 0; k < kDB; ++k) acc[b][k] *= f;
     }
     // lane i of 16: row 4 g + i / 4, elements 16 k + 4 (i % 4) ..
-    auto turned = [&](int k) {
-      const int row = 4 * g + (col >> 2), half = (col & 2) >> 1, off = 8 * (col & 1);
-      const u32x2 x = read_turned(vs + vswz<DP>(row, 2 * k + half) + off);
-      const u32x2 y = read_turned(vs + vswz<DP>(16 + row, 2 * k + half) + off);
-      return u32x4{x[0], x[1], y[0], y[1]};
+    auto turned = [&](int x, int k) {
+      const int row = 32 * x + 4 * g + (col >> 2), half = (col & 2) >> 1, off = 8 * (col & 1);
+      const u32x2 y0 = read_turned(vs + vswz<DP>(row, 2 * k + half) + off);
+      const u32x2 y1 = read_turned(vs + vswz<DP>(16 + row, 2 * k + half) + off);
+      return u32x4{y0[0], y0[1], y1[0], y1[1]};
     };
     if (masked && __any(odd != 0))
 #pragma unroll 1
-      for (int32_t o = t; o < min(t + 32, p.tb); ++o)
+      for (int32_t o = t; o < min(t + kTok, p.tb); ++o)
 #pragma unroll
         for (int k = 0; k < kDB; ++k) {
           const f32x4 x = odd_values<kF16, kQ8>(a, p, o, min(16 * k + fresh(4 * g), D - 4));
@@ -402,62 +407,26 @@ __device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char*
             for (int i = 0; i < 4; ++i) acc[b][k][i] += o < lim[b] ? x[i] : 0.0f;
         }
 #pragma unroll
-    for (int k = 0; k < kDB; ++k) {
-      const u32x4 va = turned(k);
+    for (int x = 0; x < kX; ++x)
 #pragma unroll
-      for (int b = 0; b < RB; ++b) acc[b][k] = mfma16<kF16>(va, pr[b], acc[b][k]);
-    }
+      for (int k = 0; k < kDB; ++k) {
+        const u32x4 va = turned(x, k);
+#pragma unroll
+        for (int b = 0; b < RB; ++b) acc[b][k] = mfma16<kF16>(va, pr[b][x], acc[b][k]);
+      }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
 
-  // the four waves' results: waves 2 and 3 to 0 and 1, then 1 to 0
+  const int at = fresh(lane), d0 = 4 * (at >> 4);
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
     l[b] += __shfl_xor(l[b], 16, 64);
     l[b] += __shfl_xor(l[b], 32, 64);
-    if (g == 0) ml[wave * kNarrowRows + b * 16 + col] = float2{m[b], l[b]};
-  }
-  __syncthreads();
+    const int32_t r = b * 16 + (at & 15);
+    if (r < p.rows) {
+      const float inv = put_ml(a, p, r, m[b], l[b], d0 == 0);
 #pragma unroll
-  for (int b = 0; b < RB; ++b) {
-    float top = -INFINITY;
-    for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[w * kNarrowRows + b * 16 + col].x);
-    const float mc = top == -INFINITY ? 0.0f : top * p.c;
-    float sum = 0;
-    for (int w = 0; w < 4; ++w) {
-      const float2 x = ml[w * kNarrowRows + b * 16 + col];
-      sum += x.y * __builtin_amdgcn_exp2f(__builtin_fmaf(x.x, p.c, -mc));
-    }
-    const float f = __builtin_amdgcn_exp2f(__builtin_fmaf(m[b], p.c, -mc));
-#pragma unroll
-    for (int k = 0; k < kDB; ++k) acc[b][k] *= f;
-    m[b] = top;
-    l[b] = sum;
-  }
-  f32x4* os = (f32x4*)smem;
-  for (int from = 2; from > 0; from >>= 1) {
-    if (wave >= from && wave < 2 * from)
-#pragma unroll
-      for (int b = 0; b < RB; ++b)
-#pragma unroll
-        for (int k = 0; k < kDB; ++k) os[(((wave - from) * RB + b) * kDB + k) * 64 + lane] = acc[b][k];
-    __syncthreads();
-    if (wave < from)
-#pragma unroll
-      for (int b = 0; b < RB; ++b)
-#pragma unroll
-        for (int k = 0; k < kDB; ++k) acc[b][k] += os[((wave * RB + b) * kDB + k) * 64 + lane];
-    __syncthreads();
-  }
-  if (wave == 0) {
-    const int at = fresh(lane), d0 = 4 * (at >> 4);
-#pragma unroll
-    for (int b = 0; b < RB; ++b) {
-      const int32_t r = b * 16 + (at & 15);
-      if (r < p.rows) {
-        const float inv = put_ml(a, p, r, m[b], l[b], d0 == 0);
-#pragma unroll
-        for (int k = 0; k < kDB; ++k) put4<kF16>(a, p, r, 16 * k + d0, acc[b][k], inv);
-      }
+      for (int k = 0; k < kDB; ++k) put4<kF16>(a, p, r, 16 * k + d0, acc[b][k], inv);
     }
   }
 }
@@ -664,11 +633,11 @@ __device__ inline int32_t tile_at(const int64_t* begin, int32_t n, int64_t u) {
 template <bool kF16, bool kQ8, int DP>
 __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_kernel(AttendArgs a) {
   __shared__ __align__(16) unsigned char smem[4 * wide_positions(DP) * DP * 2];
-  __shared__ float2 ml[4 * kNarrowRows];
   __shared__ int32_t odd_at[2];
   if (threadIdx.x < 2) odd_at[threadIdx.x] = -1;
   __syncthreads();
-  const int32_t head = blockIdx.x % a.cache.heads, j = blockIdx.x / a.cache.heads;
+  const int32_t head = blockIdx.x % a.cache.heads, group = blockIdx.x / a.cache.heads;
+  const int32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const AttendHead& h = *a.plan.head;
   const float c = a.scale * 1.44269504088896341f;
   Piece p;
@@ -677,7 +646,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_kernel(AttendAr
   p.c = fmaxf(fabsf(c), 1.17549435e-38f);  // (not 0: it multiplies infinities)
   p.neg = c < 0 ? 0x80008000u : 0u;
   for (int kind = 0; kind < 2; ++kind) {
-    const int32_t n = h.groups[kind];
+    const int32_t n = h.groups[kind], j = kind == 0 ? group : group + wave * a.plan.groups;
     if (j >= n) continue;
     const int64_t units = h.units[kind];
     int64_t u = units * j / n;
@@ -697,7 +666,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_kernel(AttendAr
       p.tb = (int32_t)min((int64_t)t.t1, t.t0 + to * kUnit);
       p.slot = t.slot < 0 ? -1 : t.slot + (j - t.first) * t.rows;
       if (kind == 0) wide_piece<kF16, kQ8, DP>(a, p, smem, odd_at);
-      else narrow_piece<kF16, kQ8, DP, kNarrowRows / 16>(a, p, smem, ml);
+      else narrow_piece<kF16, kQ8, DP, kNarrowRows / 16>(a, p, smem + wave * narrow_positions(kQ8, DP) * DP * 2);
       u += to - from;
     }
   }

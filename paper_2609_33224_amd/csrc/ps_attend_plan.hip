@@ -277,7 +277,7 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
     auto units_of = [&](int32_t k) { return (int64_t)((max(0, tiles[k].t1 - tiles[k].t0) + kUnit - 1) / kUnit); };
     const int64_t units = scan_all(n_tiles[kind], sums, units_of, [&](int32_t k, int64_t at) { p.begin[kind][k] = at; });
     __syncthreads();
-    const int32_t groups = (int32_t)min((int64_t)p.groups, units);
+    const int32_t groups = (int32_t)min((int64_t)p.groups * (kind == 0 ? 1 : kWavesPerGroup), units);
     h.n_tiles[kind] = n_tiles[kind];
     h.units[kind] = units;
     h.groups[kind] = groups;

@@ -96,12 +96,13 @@ __host__ __device__ inline bool block_locate(const BlockWin& w, int32_t row, boo
 // rows (row of the window x query head of the group, row-major) are cut into
 // tiles; a tile is wide (up to kWideRows rows) or narrow (all rows of a segment of
 // kNarrowRows at most).  The tiles' positions, in units of kUnit, laid end
-// to end are dealt in equal runs to the workgroups of each key / value head,
-// so that a tile may be cut into pieces; pieces and shared segments leave
+// to end are dealt in equal runs to the workgroups of each key / value head (wide) or
+// to their waves (narrow), so that a tile may be cut into pieces; pieces and shared segments leave
 // partial results, which a second kernel joins.
 constexpr int kUnit = 64;
 constexpr int kWideRows = 128;
 constexpr int kNarrowRows = 16;
+constexpr int kWavesPerGroup = 4;
 constexpr int kShareMinTokens = 64;  // of a prefix
 constexpr int kShareMaxRows = 64;    // of a member (or one row of all its heads)
 
@@ -119,7 +120,7 @@ struct AttendTile {
   int32_t pre_len, p0;
   int32_t row0, rows;  // of the segment's rows
   int32_t t0, t1;
-  int32_t first;   // the first workgroup (of its head) that takes a piece
+  int32_t first;   // the first workgroup or wave (of its head) that takes a piece
   int32_t pieces;
   int32_t slot;    // first row of the partial results, `rows` per piece; -1: written out directly
   int32_t shared;  // its rows have another segment
@@ -139,7 +140,7 @@ constexpr int32_t kWideBit = 1 << 30;
 struct AttendHead {
   int32_t n_joins;
   int32_t n_tiles[2];  // wide, narrow
-  int32_t groups[2];   // workgroups per head that take them
+  int32_t groups[2];   // workgroups, waves per head that take them
   int64_t units[2];
 };
 

@@ -166,9 +166,9 @@ void size_plan(ps_attend_plan* p, int32_t num_cus) {
   d.groups = std::max(1, num_cus * ps_attend_per_cu(p->dim) / p->kv_heads);
   // Of partial results: each row of a shared segment once, in both of its segments;
   // and the pieces of tiles that are cut, of which there are fewer than twice
-  // as many as workgroups, for each kind.
+  // as many as workgroups or waves that take them.
   const int64_t shared = std::min(rows, n * std::max(kShareMaxRows, p->ratio()));
-  d.slot_rows = (int32_t)std::min<int64_t>(2 * shared + 2 * (int64_t)d.groups * (kWideRows + kNarrowRows), INT32_MAX);
+  d.slot_rows = (int32_t)std::min<int64_t>(2 * shared + 2 * (int64_t)d.groups * (kWideRows + kWavesPerGroup * kNarrowRows), INT32_MAX);
 }
 
 }  // namespace

@@ -33,11 +33,11 @@ __device__ inline float element(const u32x4& x, int j) {
 }
 
 // A wave takes `per` rows (kMaxPer at most): a lane each finds where they lie, and the
-// wave then moves their units (a head's K or V of a row, LP lanes), kAtOnce
+// wave then moves their units (a head's K or V of a row, LP lanes), several
 // steps of 64 lanes at a time, so that the lookups' latency is paid once per wave and several
 // loads are in flight.
 constexpr int kMaxPer = 8;
-constexpr int kAtOnce = 4;
+constexpr int kWriteAtOnce = 4, kReadAtOnce = 8;  // (the other way round: 93 -> 108 us and 132 -> 146 us)
 
 struct Place {
   int64_t page;
@@ -99,11 +99,11 @@ __global__ __launch_bounds__(kBlock) void write_kernel(BlockCache c, BlockWin w,
   if (first >= w.n_rows) return;
   const int32_t row0 = (int32_t)first, steps = (per * 2 * c.heads * LP + 63) / 64;
   const Place mine = place_of(w, row0, per);
-  for (int32_t s0 = 0; s0 < steps; s0 += kAtOnce) {
-    Unit u[kAtOnce];
-    u32x4 x[kAtOnce];
+  for (int32_t s0 = 0; s0 < steps; s0 += kWriteAtOnce) {
+    Unit u[kWriteAtOnce];
+    u32x4 x[kWriteAtOnce];
 #pragma unroll
-    for (int i = 0; i < kAtOnce; ++i) {
+    for (int i = 0; i < kWriteAtOnce; ++i) {
       u[i] = unit_of<LP>(c, mine, row0, per, s0 + i);
       x[i] = u32x4{0, 0, 0, 0};
       const BlockRows& src = u[i].v ? v : k;
@@ -111,7 +111,7 @@ __global__ __launch_bounds__(kBlock) void write_kernel(BlockCache c, BlockWin w,
         x[i] = *(const u32x4*)(src.data + 2 * (u[i].row * src.row + u[i].head * src.head + u[i].d));
     }
 #pragma unroll
-    for (int i = 0; i < kAtOnce; ++i) {
+    for (int i = 0; i < kWriteAtOnce; ++i) {
       const bool put = u[i].state == 2 && u[i].d < c.dim;
       unsigned char* dst = u[i].v ? c.v : c.k;
       if (!kQuant) {
@@ -155,12 +155,12 @@ __global__ __launch_bounds__(kBlock) void read_kernel(BlockCache c, BlockWin w, 
   if (first >= w.n_rows) return;
   const int32_t row0 = (int32_t)first, steps = (per * 2 * c.heads * LP + 63) / 64;
   const Place mine = place_of(w, row0, per);
-  for (int32_t s0 = 0; s0 < steps; s0 += kAtOnce) {
-    Unit u[kAtOnce];
-    u32x4 x[kAtOnce];
-    uint32_t ex[kAtOnce];
+  for (int32_t s0 = 0; s0 < steps; s0 += kReadAtOnce) {
+    Unit u[kReadAtOnce];
+    u32x4 x[kReadAtOnce];
+    uint32_t ex[kReadAtOnce];
 #pragma unroll
-    for (int i = 0; i < kAtOnce; ++i) {
+    for (int i = 0; i < kReadAtOnce; ++i) {
       u[i] = unit_of<LP>(c, mine, row0, per, s0 + i);
       x[i] = u32x4{0, 0, 0, 0};
       ex[i] = 127;
@@ -177,7 +177,7 @@ __global__ __launch_bounds__(kBlock) void read_kernel(BlockCache c, BlockWin w, 
       }
     }
 #pragma unroll
-    for (int i = 0; i < kAtOnce; ++i) {
+    for (int i = 0; i < kReadAtOnce; ++i) {
       u32x4 o = x[i];
       if (kQuant) {
         const float s = __builtin_bit_cast(float, ex[i] << 23);
@@ -195,7 +195,7 @@ __global__ __launch_bounds__(kBlock) void read_kernel(BlockCache c, BlockWin w, 
       }
       const BlockRows& dst = u[i].v ? v : k;
       if (u[i].state > 0 && u[i].d < c.dim)
-        *(u32x4*)(dst.data + 2 * (u[i].row * dst.row + u[i].head * dst.head + u[i].d)) = o;
+        __builtin_nontemporal_store(o, (u32x4*)(dst.data + 2 * (u[i].row * dst.row + u[i].head * dst.head + u[i].d)));  // (132 -> 124 us)
     }
   }
 }
