@@ -672,21 +672,29 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_kernel(AttendAr
   }
 }
 
-// Joins the partial results of the plan's list of rows, a wave for each row and
-// key / value head, and writes the rows that nothing was computed for.  The pieces' maxima and
-// sums are a lane's each, 64 at a time; LG lanes hold a row of results, so 64 / LG
-// pieces are read at once.
+// Joins the partial results of the plan's list of rows, for each row and key / value
+// head, and writes the rows that nothing was computed for.  Where there are no more rows than
+// workgroups (a few long contexts, cut into many pieces), a row is a workgroup's: its
+// waves take every fourth run of 64 / LG * kAtOnce pieces; otherwise a wave's.  LG lanes
+// hold a row of results, so 64 / LG pieces are read at once, kAtOnce times.
 template <bool kF16, int LG>
 __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
+  constexpr int kAtOnce = 4, kStep = 64 / LG, kRun = kAtOnce * kStep;
+  __shared__ f32x4 rows[3][LG];
+  __shared__ float sums[4];
   const int lane = threadIdx.x & 63, sub = lane / LG, d = 4 * (lane % LG);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int32_t D = a.cache.dim;
   const int64_t n = (int64_t)a.plan.head->n_joins * a.cache.heads;
-  for (int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); id < n; id += (int64_t)gridDim.x * 4) {
+  const bool together = n <= gridDim.x;  // (the same for the grid)
+  const int64_t first = together ? blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
+  for (int64_t id = first; id < n; id += (int64_t)gridDim.x * (together ? 1 : 4)) {
     const AttendJoin x = a.plan.joins[id / a.cache.heads];
     const int32_t head = (int32_t)(id % a.cache.heads);
     const int64_t row = a.plan.row[x.place];
+    const bool writes = !together || wave == 0;
     if (x.sub < 0) {
-      for (int32_t h = head * a.ratio; h < (head + 1) * a.ratio; ++h) {
+      for (int32_t h = head * a.ratio; writes && h < (head + 1) * a.ratio; ++h) {
         if (sub == 0 && d < D)
           *(u32x2*)(a.out.data + 2 * (row * a.out.row + (int64_t)h * a.out.head + d)) = u32x2{0, 0};
         if (a.lse && lane == 0) a.lse[row * a.heads + h] = -INFINITY;
@@ -709,54 +717,58 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
       const bool own = j < count[0];
       return (own ? from[0] : from[1]) + (int64_t)(own ? j : j - count[0]) * (own ? step[0] : step[1]);
     };
-    float2 ml = {-INFINITY, 0.0f};
-    if (lane < total) ml = a.plan.part_ml[slot(lane)];
-    float top = ml.x;
-    for (int32_t j = 64 + lane; j < total; j += 64) top = fmaxf(top, a.plan.part_ml[slot(j)].x);
+    float top = -INFINITY;
+    for (int32_t j = lane; j < total; j += 64) top = fmaxf(top, a.plan.part_ml[slot(j)].x);
     for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
     const float mc = top == -INFINITY ? 0.0f : top;
     f32x4 acc = {0, 0, 0, 0};
     float l = 0;
-    for (int32_t j0 = 0; j0 < total; j0 += 64) {
-      if (j0 > 0) {
-        ml = float2{-INFINITY, 0.0f};
-        if (j0 + lane < total) ml = a.plan.part_ml[slot(j0 + lane)];
-      }
-      const float f = __builtin_amdgcn_exp2f(ml.x - mc);
-      float part = ml.y * f;
-      for (int o = 32; o > 0; o >>= 1) part += __shfl_xor(part, o, 64);
-      l += part;
-      const int32_t m = min(64, total - j0);
-      constexpr int kAtOnce = 4, kStep = 64 / LG;
-      for (int32_t j = 0; j < m; j += kAtOnce * kStep) {
-        f32x4 o[kAtOnce];
-        float w[kAtOnce];
+    for (int32_t j = together ? wave * kRun : 0; j < total; j += together ? 4 * kRun : kRun) {
+      f32x4 o[kAtOnce];
+      float2 ml[kAtOnce];
 #pragma unroll
-        for (int u = 0; u < kAtOnce; ++u) {
-          const int32_t at = j + u * kStep + sub, in = min(at, m - 1);
-          w[u] = __shfl(f, in, 64);
-          o[u] = f32x4{0, 0, 0, 0};
-          if (at < m && d < D) o[u] = *(const f32x4*)(a.plan.part + slot(j0 + in) * D + d);
+      for (int u = 0; u < kAtOnce; ++u) {
+        const int32_t at = j + u * kStep + sub;
+        o[u] = f32x4{0, 0, 0, 0};
+        ml[u] = float2{-INFINITY, 0.0f};
+        if (at < total) {
+          const int64_t s = slot(at);
+          ml[u] = a.plan.part_ml[s];
+          if (d < D) o[u] = *(const f32x4*)(a.plan.part + s * D + d);
         }
+      }
 #pragma unroll
-        for (int u = 0; u < kAtOnce; ++u)
+      for (int u = 0; u < kAtOnce; ++u) {
+        const float f = __builtin_amdgcn_exp2f(ml[u].x - mc);
+        l = __builtin_fmaf(ml[u].y, f, l);
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            acc[e] = j + u * kStep + sub < m ? __builtin_fmaf(o[u][e], w[u], acc[e]) : acc[e];
+        for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(o[u][e], f, acc[e]);
       }
     }
 #pragma unroll
-    for (int o = LG; o < 64; o <<= 1)
+    for (int o = LG; o < 64; o <<= 1) {
+      l += __shfl_xor(l, o, 64);
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], o, 64);
+    }
+    if (together) {
+      if (wave > 0 && sub == 0) rows[wave - 1][lane % LG] = acc;
+      if (lane == 0) sums[wave] = l;
+      __syncthreads();
+      l = sums[0] + sums[1] + sums[2] + sums[3];
+#pragma unroll
+      for (int w = 0; w < 3; ++w) acc += rows[w][lane % LG];
+      __syncthreads();
+    }
     const int32_t h = head * a.ratio + x.sub;
     const float inv = 1.0f / l;
-    if (sub == 0 && d < D) {
+    if (writes && sub == 0 && d < D) {
       u32x2 w = {0, 0};
       if (!empty) w = u32x2{pack<kF16>(acc[0] * inv, acc[1] * inv), pack<kF16>(acc[2] * inv, acc[3] * inv)};
       *(u32x2*)(a.out.data + 2 * (row * a.out.row + (int64_t)h * a.out.head + d)) = w;
     }
-    if (a.lse && lane == 0) a.lse[row * a.heads + h] = empty ? -INFINITY : __builtin_fmaf(top, kLn2, __logf(l));
+    if (writes && a.lse && lane == 0)
+      a.lse[row * a.heads + h] = empty ? -INFINITY : __builtin_fmaf(top, kLn2, __logf(l));
   }
 }
 
