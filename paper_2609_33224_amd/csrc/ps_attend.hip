@@ -182,12 +182,11 @@ __device__ inline f32x4 odd_values(const AttendArgs& a, const Piece& p, int32_t 
   return o;
 }
 
-// Eight elements of a row of q, from element d.
-__device__ inline u32x4 load_q(const AttendArgs& a, const Piece& p, int32_t r, int32_t d) {
+// Eight elements of the row of q that begins at `at`, from element d.
+__device__ inline u32x4 load_q(const AttendArgs& a, const Piece& p, int64_t at, bool has, int32_t d) {
   u32x4 x = {0, 0, 0, 0};
-  if (r < p.rows && d < a.cache.dim) {
-    const RowAt at = row_at(a, p, r);
-    x = *(const u32x4*)(a.q.data + 2 * ((int64_t)a.plan.row[at.place] * a.q.row + (int64_t)at.head * a.q.head + d));
+  if (has && d < a.cache.dim) {
+    x = *(const u32x4*)(a.q.data + 2 * (at + d));
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] ^= p.neg;
   }
@@ -248,19 +247,6 @@ __device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char*
   const int lane = fresh(threadIdx.x & 63), col = lane & 15, g = lane >> 4;
   const int D = a.cache.dim;
 
-  u32x4 q[RB][kSteps];
-  int32_t lim[RB], least = INT32_MAX;
-#pragma unroll
-  for (int b = 0; b < RB; ++b) {
-    const int32_t r = b * 16 + col;
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s)
-      q[b][s] = load_q(a, p, r, kQ8 ? 64 * (s >> 1) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g);
-    lim[b] = r < p.rows ? a.plan.lim[row_at(a, p, r).place] : INT32_MAX;
-    least = min(least, lim[b]);
-  }
-  for (int o = 8; o > 0; o >>= 1) least = min(least, __shfl_xor(least, o, 64));
-
   f32x4 acc[RB][kDB];
   float m[RB], l[RB];
 #pragma unroll
@@ -299,9 +285,32 @@ __device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char*
     }
   };
 
+  // Pages and rows are asked for together, then keys and values, then q: loads return
+    // in order, so that a wait for q's would hold the others back.
+  u32x4 q[RB][kSteps];
+  int32_t lim[RB], least = INT32_MAX;
+  int64_t qat[RB];
   pages(p.ta);
+#pragma unroll
+  for (int b = 0; b < RB; ++b) {
+    const int32_t r = b * 16 + col;
+    const RowAt at = row_at(a, p, min(r, p.rows - 1));
+    lim[b] = a.plan.lim[at.place];
+    qat[b] = a.plan.row[at.place] * a.q.row + (int64_t)at.head * a.q.head;
+  }
   loads(p.ta);
   pages(p.ta + kTok);
+#pragma unroll
+  for (int b = 0; b < RB; ++b) {
+    const bool has = b * 16 + col < p.rows;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+      q[b][s] = load_q(a, p, qat[b], has, kQ8 ? 64 * (s >> 1) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g);
+    if (!has) lim[b] = INT32_MAX;
+    least = min(least, lim[b]);
+  }
+  for (int o = 8; o > 0; o >>= 1) least = min(least, __shfl_xor(least, o, 64));
+
   for (int32_t t = p.ta; t < p.tb; t += kTok) {
     // Values into shared memory.  Where a row may not see all of the step's, their
     // infinities and NaN are taken out, since a weight of 0 would not take them
@@ -455,13 +464,6 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
   const int32_t r = wave * 32 + col;
   const bool idle = wave * 32 >= p.rows;
 
-  u32x4 q[kSteps];
-#pragma unroll
-  for (int s = 0; s < kSteps; ++s) q[s] = load_q(a, p, r, 16 * s + 8 * hb);
-  const int32_t lim = r < p.rows ? a.plan.lim[row_at(a, p, r).place] : INT32_MAX;
-  int32_t least = lim;
-  for (int o = 16; o > 0; o >>= 1) least = min(least, __shfl_xor(least, o, 64));
-
   f32x16 acc[kDB];
 #pragma unroll
   for (int k = 0; k < kDB; ++k)
@@ -520,9 +522,19 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
     if (odd) odd_at[buf] = t;  // (a value left by another piece only costs a look)
   };
 
+  // (the order: as in the narrow kernel)
   pages(p.ta);
+  const RowAt qrow = row_at(a, p, min(r, p.rows - 1));
+  int32_t lim = a.plan.lim[qrow.place];
+  const int64_t qat = a.plan.row[qrow.place] * a.q.row + (int64_t)qrow.head * a.q.head;
   loads(p.ta);
   pages(p.ta + kTok);
+  u32x4 q[kSteps];
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s) q[s] = load_q(a, p, qat, r < p.rows, 16 * s + 8 * hb);
+  if (r >= p.rows) lim = INT32_MAX;
+  int32_t least = lim;
+  for (int o = 16; o > 0; o >>= 1) least = min(least, __shfl_xor(least, o, 64));
   stage(0, p.ta);
   __syncthreads();
   int buf = 0;
@@ -617,19 +629,6 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
   }
 }
 
-// The last of n tiles that begins at or before unit u, by the whole wave.
-__device__ inline int32_t tile_at(const int64_t* begin, int32_t n, int64_t u) {
-  const int lane = threadIdx.x & 63;
-  int32_t a = 0, b = n;  // begin[a] <= u
-  while (b - a > 1) {
-    const int32_t step = (b - a + 63) / 64, i = a + lane * step;
-    const int32_t hits = __popcll(__ballot(i < b && begin[i] <= u));
-    a += (hits - 1) * step;
-    b = min(b, a + step);
-  }
-  return a;
-}
-
 template <bool kF16, bool kQ8, int DP>
 __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_kernel(AttendArgs a) {
   __shared__ __align__(16) unsigned char smem[4 * wide_positions(DP) * DP * 2];
@@ -638,7 +637,6 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_kernel(AttendAr
   __syncthreads();
   const int32_t head = blockIdx.x % a.cache.heads, group = blockIdx.x / a.cache.heads;
   const int32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const AttendHead& h = *a.plan.head;
   const float c = a.scale * 1.44269504088896341f;
   Piece p;
   p.chain.pages = a.win.pages;
@@ -646,15 +644,11 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_kernel(AttendAr
   p.c = fmaxf(fabsf(c), 1.17549435e-38f);  // (not 0: it multiplies infinities)
   p.neg = c < 0 ? 0x80008000u : 0u;
   for (int kind = 0; kind < 2; ++kind) {
-    const int32_t n = h.groups[kind], j = kind == 0 ? group : group + wave * a.plan.groups;
-    if (j >= n) continue;
-    const int64_t units = h.units[kind];
-    int64_t u = units * j / n;
-    const int64_t end = units * (j + 1) / n;
-    for (int32_t k = tile_at(a.plan.begin[kind], h.n_tiles[kind], u); u < end; ++k) {
+    const AttendRun run = a.plan.runs[kind][kind == 0 ? group : group + wave * a.plan.groups];
+    int32_t from = run.from, left = run.units;
+    for (int32_t k = run.tile; left > 0; ++k, from = 0) {
       const AttendTile t = a.plan.tiles[kind][k];
-      const int64_t from = u - a.plan.begin[kind][k];
-      const int64_t len = max(0, (t.t1 - t.t0 + kUnit - 1) / kUnit), to = min(len, from + (end - u));
+      const int32_t len = max(0, (t.t1 - t.t0 + kUnit - 1) / kUnit), to = min(len, from + left);
       if (to <= from) continue;  // (a tile of no positions)
       p.chain.pre_off = t.pre_off;
       p.chain.tail_off = t.tail_off;
@@ -662,12 +656,12 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_kernel(AttendAr
       p.p0 = t.p0;
       p.row0 = t.row0;
       p.rows = t.rows;
-      p.ta = t.t0 + (int32_t)(from * kUnit);
-      p.tb = (int32_t)min((int64_t)t.t1, t.t0 + to * kUnit);
-      p.slot = t.slot < 0 ? -1 : t.slot + (j - t.first) * t.rows;
+      p.ta = t.t0 + from * kUnit;
+      p.tb = min(t.t1, t.t0 + to * kUnit);
+      p.slot = t.slot < 0 ? -1 : t.slot + (run.number - t.first) * t.rows;
       if (kind == 0) wide_piece<kF16, kQ8, DP>(a, p, smem, odd_at);
       else narrow_piece<kF16, kQ8, DP, kNarrowRows / 16>(a, p, smem + wave * narrow_positions(kQ8, DP) * DP * 2);
-      u += to - from;
+      left -= to - from;
     }
   }
 }

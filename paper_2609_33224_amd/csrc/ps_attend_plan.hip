@@ -68,10 +68,15 @@ __device__ inline int64_t scan_all(int32_t n, int64_t* lds, V value, S store) {
   return total;
 }
 
-// The workgroup (of n that share `units` in equal runs) that takes unit u:
-// the largest j with floor(j units / n) <= u.
-__device__ inline int32_t taker(int64_t u, int64_t units, int32_t n) {
-  return (int32_t)(((u + 1) * n + units - 1) / units - 1);
+// The workgroup or wave that takes unit u: the largest one that begins at or before it.
+__device__ inline int32_t taker(const AttendHead& h, int kind, int64_t u) {
+  int32_t a = 0, b = runs_of(h, kind);
+  while (b - a > 1) {
+    const int32_t m = (a + b) >> 1;
+    if (run_begin(h, kind, m) <= u) a = m;
+    else b = m;
+  }
+  return a;
 }
 
 __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, BlockWin w, int32_t ratio,
@@ -92,6 +97,9 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
     if (d_flags)
       for (int32_t r = tid; r < n; r += kThreads) d_flags[r] = PS_R_INVALID;
     if (tid == 0) *p.head = AttendHead{};
+    for (int kind = 0; kind < 2; ++kind)
+      for (int32_t j = tid; j < p.groups * (kind == 0 ? 1 : kWavesPerGroup); j += kThreads)
+        p.runs[kind][j] = AttendRun{0, 0, 0, 0};
     return;
   }
 
@@ -270,21 +278,49 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
   __syncthreads();
 
   // Units end to end, who takes them, and the rows of partial results.
-  int64_t slots = 0;
   AttendHead h{};
+  auto units_of = [&](const AttendTile& t) { return (int64_t)((max(0, t.t1 - t.t0) + kUnit - 1) / kUnit); };
+  for (int kind = 0; kind < 2; ++kind) {
+    h.n_tiles[kind] = n_tiles[kind];
+    h.units[kind] = scan_all(
+        n_tiles[kind], sums, [&](int32_t k) { return units_of(p.tiles[kind][k]); },
+        [&](int32_t k, int64_t at) { p.begin[kind][k] = at; });
+  }
+  h.groups = (int32_t)min((int64_t)p.groups, h.units[0] + h.units[1]);
+  __syncthreads();
+  int64_t slots = 0;
   for (int kind = 0; kind < 2; ++kind) {
     AttendTile* tiles = p.tiles[kind];
-    auto units_of = [&](int32_t k) { return (int64_t)((max(0, tiles[k].t1 - tiles[k].t0) + kUnit - 1) / kUnit); };
-    const int64_t units = scan_all(n_tiles[kind], sums, units_of, [&](int32_t k, int64_t at) { p.begin[kind][k] = at; });
+    // (the waves' runs lie wave by wave of all workgroups)
+    const int32_t per = kind == 0 ? 1 : kWavesPerGroup;
+    auto run_at = [&](int32_t x) -> AttendRun& { return p.runs[kind][x / per + x % per * p.groups]; };
+    for (int32_t x = tid; x < p.groups * per; x += kThreads) {
+      AttendRun run{0, 0, 0, 0};
+      if (x < h.groups * per) {
+        const int64_t at = run_begin(h, kind, x);
+        run.units = (int32_t)min(run_begin(h, kind, x + 1) - at, (int64_t)INT32_MAX);
+        if (run.units > 0) {
+          int32_t a = 0, b = n_tiles[kind];  // the last tile that begins at or before `at`
+          while (b - a > 1) {
+            const int32_t m = (a + b) >> 1;
+            if (p.begin[kind][m] <= at) a = m;
+            else b = m;
+          }
+          run.tile = a;
+          run.from = (int32_t)(at - p.begin[kind][a]);
+        }
+      }
+      run_at(x) = run;
+    }
     __syncthreads();
-    const int32_t groups = (int32_t)min((int64_t)p.groups * (kind == 0 ? 1 : kWavesPerGroup), units);
-    h.n_tiles[kind] = n_tiles[kind];
-    h.units[kind] = units;
-    h.groups[kind] = groups;
+    scan_all(
+        h.groups * per, sums, [&](int32_t x) { return (int64_t)(run_at(x).units > 0); },
+        [&](int32_t x, int64_t at) { run_at(x).number = (int32_t)at; });
+    __syncthreads();
     for (int32_t k = tid; k < n_tiles[kind]; k += kThreads) {
-      const int64_t u = units_of(k), b = p.begin[kind][k];
-      tiles[k].first = u > 0 ? taker(b, units, groups) : 0;
-      tiles[k].pieces = u > 0 ? taker(b + u - 1, units, groups) - tiles[k].first + 1 : 0;
+      const int64_t u = units_of(tiles[k]), b = p.begin[kind][k];
+      tiles[k].first = u > 0 ? run_at(taker(h, kind, b)).number : 0;
+      tiles[k].pieces = u > 0 ? run_at(taker(h, kind, b + u - 1)).number - tiles[k].first + 1 : 0;
     }
     __syncthreads();
     const int64_t before = slots;

@@ -95,14 +95,18 @@ __host__ __device__ inline bool block_locate(const BlockWin& w, int32_t row, boo
 // all of them, or what is left of one request's chain with its own rows.  Its
 // rows (row of the window x query head of the group, row-major) are cut into
 // tiles; a tile is wide (up to kWideRows rows) or narrow (all rows of a segment of
-// kNarrowRows at most).  The tiles' positions, in units of kUnit, laid end
-// to end are dealt in equal runs to the workgroups of each key / value head (wide) or
-// to their waves (narrow), so that a tile may be cut into pieces; pieces and shared segments leave
+// kNarrowRows at most).  The tiles' positions, in units of kUnit, are laid end
+// to end, the wide ones first, and dealt in runs of equal cost to the workgroups of
+// each key / value head (the narrow ones of a workgroup in equal runs to its waves), so
+// that a tile may be cut into pieces; pieces and shared segments leave
 // partial results, which a second kernel joins.
 constexpr int kUnit = 64;
 constexpr int kWideRows = 128;
 constexpr int kNarrowRows = 16;
 constexpr int kWavesPerGroup = 4;
+// Cost of a unit for a workgroup: 2.9 us of a wide tile's, 1.5 (8 bits) to 3.0 us (16
+// bits) of a narrow one's, with every workgroup at work.
+constexpr int kWideCost = 3, kNarrowCost = 2;
 constexpr int kShareMinTokens = 64;  // of a prefix
 constexpr int kShareMaxRows = 64;    // of a member (or one row of all its heads)
 
@@ -120,7 +124,7 @@ struct AttendTile {
   int32_t pre_len, p0;
   int32_t row0, rows;  // of the segment's rows
   int32_t t0, t1;
-  int32_t first;   // the first workgroup or wave (of its head) that takes a piece
+  int32_t first;   // number of the first run that takes a piece of it
   int32_t pieces;
   int32_t slot;    // first row of the partial results, `rows` per piece; -1: written out directly
   int32_t shared;  // its rows have another segment
@@ -140,8 +144,37 @@ constexpr int32_t kWideBit = 1 << 30;
 struct AttendHead {
   int32_t n_joins;
   int32_t n_tiles[2];  // wide, narrow
-  int32_t groups[2];   // workgroups, waves per head that take them
+  int32_t groups;      // workgroups per head that have something to do
   int64_t units[2];
+};
+
+// The first wide unit of workgroup j; the first narrow unit of wave x (4 to a workgroup).
+__host__ __device__ inline int64_t wide_begin(const AttendHead& h, int64_t j) {
+  const int64_t cost = (kWideCost * h.units[0] + kNarrowCost * h.units[1]) * j / h.groups;
+  const int64_t u = (cost + kWideCost - 1) / kWideCost;
+  return u < h.units[0] ? u : h.units[0];
+}
+__host__ __device__ inline int64_t group_narrow_begin(const AttendHead& h, int64_t j) {
+  const int64_t wide = kWideCost * h.units[0], cost = (wide + kNarrowCost * h.units[1]) * j / h.groups;
+  const int64_t u = cost <= wide ? 0 : (cost - wide + kNarrowCost - 1) / kNarrowCost;
+  return u < h.units[1] ? u : h.units[1];
+}
+__host__ __device__ inline int64_t narrow_begin(const AttendHead& h, int64_t x) {
+  const int64_t j = x / kWavesPerGroup, a = group_narrow_begin(h, j);
+  return a + (group_narrow_begin(h, j + 1) - a) * (x % kWavesPerGroup) / kWavesPerGroup;
+}
+__host__ __device__ inline int64_t run_begin(const AttendHead& h, int kind, int64_t j) {
+  return kind == 0 ? wide_begin(h, j) : narrow_begin(h, j);
+}
+__host__ __device__ inline int32_t runs_of(const AttendHead& h, int kind) {
+  return kind == 0 ? h.groups : h.groups * kWavesPerGroup;
+}
+
+// Where a workgroup's or wave's run begins and ends.
+struct alignas(16) AttendRun {
+  int32_t tile, from;  // first tile, the first unit of it
+  int32_t units;       // in all; 0: nothing to do
+  int32_t number;      // among those of the head that have something to do
 };
 
 struct AttendPlanDev {
@@ -161,6 +194,7 @@ struct AttendPlanDev {
   AttendSeg* segs;    // 2 per place: prefix (first members only), own
   AttendTile* tiles[2];
   int64_t* begin[2];  // first unit of each tile
+  AttendRun* runs[2];  // of each workgroup of a head; of each wave, wave by wave of all workgroups
   AttendJoin* joins;
   float* part;        // partial results: [head][slot rows][dim], weights as numerators
   float2* part_ml;    // their maxima (times scale * log2 e) and sums
