@@ -115,6 +115,12 @@ __device__ inline u32x2 read_turned(const unsigned char* p) {
 
 __device__ inline float scale_of(uint32_t x) { return __builtin_bit_cast(float, x << 23); }
 
+// A value that is the same for the wave, as a scalar.
+__device__ inline int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ inline int64_t uniform(int64_t x) {
+  return (int64_t)((uint64_t)(uint32_t)uniform((int32_t)(x >> 32)) << 32 | (uint32_t)uniform((int32_t)x));
+}
+
 // The chain of a tile, with what it takes to find a position's bytes.
 struct Chain {
   const int32_t* pages;
@@ -643,26 +649,47 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_kernel(AttendAr
   p.head = head;
   p.c = fmaxf(fabsf(c), 1.17549435e-38f);  // (not 0: it multiplies infinities)
   p.neg = c < 0 ? 0x80008000u : 0u;
-  for (int kind = 0; kind < 2; ++kind) {
-    const AttendRun run = a.plan.runs[kind][kind == 0 ? group : group + wave * a.plan.groups];
-    int32_t from = run.from, left = run.units;
-    for (int32_t k = run.tile; left > 0; ++k, from = 0) {
-      const AttendTile t = a.plan.tiles[kind][k];
-      const int32_t len = max(0, (t.t1 - t.t0 + kUnit - 1) / kUnit), to = min(len, from + left);
-      if (to <= from) continue;  // (a tile of no positions)
-      p.chain.pre_off = t.pre_off;
-      p.chain.tail_off = t.tail_off;
-      p.chain.pre_len = t.pre_len;
-      p.p0 = t.p0;
-      p.row0 = t.row0;
-      p.rows = t.rows;
-      p.ta = t.t0 + from * kUnit;
-      p.tb = min(t.t1, t.t0 + to * kUnit);
-      p.slot = t.slot < 0 ? -1 : t.slot + (run.number - t.first) * t.rows;
-      if (kind == 0) wide_piece<kF16, kQ8, DP>(a, p, smem, odd_at);
-      else narrow_piece<kF16, kQ8, DP, kNarrowRows / 16>(a, p, smem + wave * narrow_positions(kQ8, DP) * DP * 2);
-      left -= to - from;
+  // (scalars throughout: what is loaded after the first store would be a lane's otherwise)
+  const AttendHead& h = *a.plan.head;
+  const int32_t wide_groups = uniform(h.wide_groups);
+  const int kind = group >= wide_groups;
+  // (the waves' runs go round the workgroups)
+  const int32_t r = kind == 0 ? group : group - wide_groups + wave * (a.plan.groups - wide_groups);
+  if (r >= uniform(h.runs[kind])) return;  // (of a wide tile's workgroup, all waves or none)
+  const AttendRun run = a.plan.runs[kind][r];
+  const int32_t rounds = kind == 0 ? uniform(h.rounds) : 0, number = uniform(run.number);
+  int32_t next = uniform(run.tile), at = uniform(run.from), left = uniform(run.units);
+  for (int32_t round = 0;;) {
+    int32_t k, from, most, piece;
+    if (round < rounds) {
+      k = r + round++ * wide_groups;
+      from = piece = 0;
+      most = INT32_MAX;
+    } else {
+      if (left <= 0) break;
+      k = next++;
+      from = at;
+      most = left;
+      piece = number;
+      at = 0;
     }
+    const AttendTile* tiles = a.plan.tiles[kind];
+    const AttendTile t = tiles[k];
+    const int32_t t0 = uniform(t.t0), t1 = uniform(t.t1), slot = uniform(t.slot);
+    const int32_t n = min(max(0, (t1 - t0 + kUnit - 1) / kUnit) - from, most);
+    if (n <= 0) continue;  // (a tile of no positions)
+    p.chain.pre_off = uniform(t.pre_off);
+    p.chain.tail_off = uniform(t.tail_off);
+    p.chain.pre_len = uniform(t.pre_len);
+    p.p0 = uniform(t.p0);
+    p.row0 = uniform(t.row0);
+    p.rows = uniform(t.rows);
+    p.ta = t0 + from * kUnit;
+    p.tb = min(t1, t0 + (from + n) * kUnit);
+    p.slot = slot < 0 ? -1 : slot + (piece - uniform(t.first)) * p.rows;
+    if (kind == 0) wide_piece<kF16, kQ8, DP>(a, p, smem, odd_at);
+    else narrow_piece<kF16, kQ8, DP, kNarrowRows / 16>(a, p, smem + wave * narrow_positions(kQ8, DP) * DP * 2);
+    if (most != INT32_MAX) left -= n;
   }
 }
 

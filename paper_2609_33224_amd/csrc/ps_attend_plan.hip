@@ -68,17 +68,6 @@ __device__ inline int64_t scan_all(int32_t n, int64_t* lds, V value, S store) {
   return total;
 }
 
-// The workgroup or wave that takes unit u: the largest one that begins at or before it.
-__device__ inline int32_t taker(const AttendHead& h, int kind, int64_t u) {
-  int32_t a = 0, b = runs_of(h, kind);
-  while (b - a > 1) {
-    const int32_t m = (a + b) >> 1;
-    if (run_begin(h, kind, m) <= u) a = m;
-    else b = m;
-  }
-  return a;
-}
-
 __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, BlockWin w, int32_t ratio,
                                                             uint32_t* d_flags) {
   __shared__ uint32_t keys[PS_MAX_WINDOW_REQ];
@@ -97,9 +86,6 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
     if (d_flags)
       for (int32_t r = tid; r < n; r += kThreads) d_flags[r] = PS_R_INVALID;
     if (tid == 0) *p.head = AttendHead{};
-    for (int kind = 0; kind < 2; ++kind)
-      for (int32_t j = tid; j < p.groups * (kind == 0 ? 1 : kWavesPerGroup); j += kThreads)
-        p.runs[kind][j] = AttendRun{0, 0, 0, 0};
     return;
   }
 
@@ -279,48 +265,96 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
 
   // Units end to end, who takes them, and the rows of partial results.
   AttendHead h{};
+  int64_t units[2];
   auto units_of = [&](const AttendTile& t) { return (int64_t)((max(0, t.t1 - t.t0) + kUnit - 1) / kUnit); };
   for (int kind = 0; kind < 2; ++kind) {
     h.n_tiles[kind] = n_tiles[kind];
-    h.units[kind] = scan_all(
+    units[kind] = scan_all(
         n_tiles[kind], sums, [&](int32_t k) { return units_of(p.tiles[kind][k]); },
         [&](int32_t k, int64_t at) { p.begin[kind][k] = at; });
   }
-  h.groups = (int32_t)min((int64_t)p.groups, h.units[0] + h.units[1]);
+  {
+    const int64_t wide = kWideCost * units[0], all = wide + kNarrowCost * units[1];
+    int64_t n_wide = all > 0 ? (wide * p.groups + all / 2) / all : 0;
+    if (units[0] > 0) n_wide = max(n_wide, (int64_t)1);
+    if (units[1] > 0) n_wide = min(n_wide, (int64_t)p.groups - 1);
+    h.wide_groups = h.runs[0] = (int32_t)n_wide;
+    h.runs[1] = (int32_t)min((p.groups - n_wide) * kWavesPerGroup, units[1]);
+  }
   __syncthreads();
+  // Rounds of whole tiles, as many as leave no workgroup (a thread each) above
+  // the average; then `share` units more for each, the most evenly.
+  int64_t share = 0;
+  if (h.wide_groups > 0) {
+    const int32_t n_wide = h.wide_groups;
+    const bool mine = tid < n_wide;
+    int64_t whole = 0, total;
+    for (h.rounds = n_tiles[0] / n_wide;; --h.rounds) {
+      whole = 0;
+      for (int32_t i = 0; mine && i < h.rounds; ++i) whole += units_of(p.tiles[0][tid + i * n_wide]);
+      if (!__syncthreads_or(mine && h.rounds > 0 && whole * n_wide > units[0])) break;
+    }
+    // a level that those below it are filled up to
+    int64_t left = units[0], n_below = n_wide;
+    bool below = mine;
+    for (;;) {
+      block_scan(mine && !below ? whole : 0, &total, sums);
+      left = units[0] - total;
+      const bool out = below && whole * n_below > left;
+      block_scan(out ? 1 : 0, &total, sums);
+      if (total == 0) break;
+      n_below -= total;
+      below = below && !out;
+    }
+    // (left / n_below each, the first left % n_below one more)
+    const int64_t rank = block_scan(below ? 1 : 0, &total, sums);
+    if (below) share = left / n_below + (rank < left % n_below) - whole;
+  }
   int64_t slots = 0;
   for (int kind = 0; kind < 2; ++kind) {
     AttendTile* tiles = p.tiles[kind];
-    // (the waves' runs lie wave by wave of all workgroups)
-    const int32_t per = kind == 0 ? 1 : kWavesPerGroup;
-    auto run_at = [&](int32_t x) -> AttendRun& { return p.runs[kind][x / per + x % per * p.groups]; };
-    for (int32_t x = tid; x < p.groups * per; x += kThreads) {
-      AttendRun run{0, 0, 0, 0};
-      if (x < h.groups * per) {
-        const int64_t at = run_begin(h, kind, x);
-        run.units = (int32_t)min(run_begin(h, kind, x + 1) - at, (int64_t)INT32_MAX);
-        if (run.units > 0) {
-          int32_t a = 0, b = n_tiles[kind];  // the last tile that begins at or before `at`
-          while (b - a > 1) {
-            const int32_t m = (a + b) >> 1;
-            if (p.begin[kind][m] <= at) a = m;
-            else b = m;
-          }
-          run.tile = a;
-          run.from = (int32_t)(at - p.begin[kind][a]);
-        }
+    const int32_t whole = kind == 0 ? h.rounds * h.wide_groups : 0, runs = h.runs[kind];
+    const int64_t skip = whole < n_tiles[kind] ? p.begin[kind][whole] : units[kind];
+    if (kind == 0) {
+      int64_t total;
+      const int64_t at = block_scan(share, &total, sums), number = block_scan(share > 0, &total, sums);
+      if (tid < runs) {
+        p.run_at[0][tid] = skip + at;
+        p.runs[0][tid].units = (int32_t)share;
+        p.runs[0][tid].number = (int32_t)number;
       }
-      run_at(x) = run;
+    } else {
+      for (int32_t r = tid; r < runs; r += kThreads) {
+        p.run_at[1][r] = units[1] * r / runs;
+        p.runs[1][r].units = (int32_t)(units[1] * (r + 1) / runs - units[1] * r / runs);
+        p.runs[1][r].number = r;
+      }
     }
     __syncthreads();
-    scan_all(
-        h.groups * per, sums, [&](int32_t x) { return (int64_t)(run_at(x).units > 0); },
-        [&](int32_t x, int64_t at) { run_at(x).number = (int32_t)at; });
-    __syncthreads();
+    for (int32_t r = tid; r < runs; r += kThreads) {
+      const int64_t at = p.run_at[kind][r];
+      int32_t a = 0, b = n_tiles[kind];  // the last tile that begins at or before `at`
+      while (b - a > 1) {
+        const int32_t m = (a + b) >> 1;
+        if (p.begin[kind][m] <= at) a = m;
+        else b = m;
+      }
+      p.runs[kind][r].tile = a;
+      p.runs[kind][r].from = (int32_t)(at - p.begin[kind][a]);
+    }
+    auto run_of = [&](int64_t u) {  // the last run that begins at or before unit u
+      int32_t a = 0, b = runs;
+      while (b - a > 1) {
+        const int32_t m = (a + b) >> 1;
+        if (p.run_at[kind][m] <= u) a = m;
+        else b = m;
+      }
+      return p.runs[kind][a].number;
+    };
     for (int32_t k = tid; k < n_tiles[kind]; k += kThreads) {
       const int64_t u = units_of(tiles[k]), b = p.begin[kind][k];
-      tiles[k].first = u > 0 ? run_at(taker(h, kind, b)).number : 0;
-      tiles[k].pieces = u > 0 ? run_at(taker(h, kind, b + u - 1)).number - tiles[k].first + 1 : 0;
+      tiles[k].first = u > 0 && k >= whole ? run_of(b) : 0;
+      tiles[k].pieces = u == 0 ? 0 : k < whole ? 1 : run_of(b + u - 1) - tiles[k].first + 1;
     }
     __syncthreads();
     const int64_t before = slots;

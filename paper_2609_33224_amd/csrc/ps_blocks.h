@@ -96,10 +96,12 @@ __host__ __device__ inline bool block_locate(const BlockWin& w, int32_t row, boo
 // rows (row of the window x query head of the group, row-major) are cut into
 // tiles; a tile is wide (up to kWideRows rows) or narrow (all rows of a segment of
 // kNarrowRows at most).  The tiles' positions, in units of kUnit, are laid end
-// to end, the wide ones first, and dealt in runs of equal cost to the workgroups of
-// each key / value head (the narrow ones of a workgroup in equal runs to its waves), so
-// that a tile may be cut into pieces; pieces and shared segments leave
-// partial results, which a second kernel joins.
+// to end and dealt in runs: the wide ones' to some workgroups of each key / value
+// head, the narrow ones' to the waves of the others, so many as the costs say.  Where there
+// are more wide tiles than workgroups, these first take whole tiles, in rounds, so that
+// neighbours go over the same positions at the same time and find them in the L2 cache;
+// what is left makes their shares even.  So a tile may be cut into pieces; pieces and
+// shared segments leave partial results, which a second kernel joins.
 constexpr int kUnit = 64;
 constexpr int kWideRows = 128;
 constexpr int kNarrowRows = 16;
@@ -143,38 +145,17 @@ constexpr int32_t kWideBit = 1 << 30;
 
 struct AttendHead {
   int32_t n_joins;
-  int32_t n_tiles[2];  // wide, narrow
-  int32_t groups;      // workgroups per head that have something to do
-  int64_t units[2];
+  int32_t n_tiles[2];   // wide, narrow
+  int32_t wide_groups;  // workgroups per head that take wide tiles; the others take narrow ones
+  int32_t rounds;       // whole wide tiles that each of them takes first: its number + i wide_groups
+  int32_t runs[2];      // wide_groups; waves that take narrow ones
 };
 
-// The first wide unit of workgroup j; the first narrow unit of wave x (4 to a workgroup).
-__host__ __device__ inline int64_t wide_begin(const AttendHead& h, int64_t j) {
-  const int64_t cost = (kWideCost * h.units[0] + kNarrowCost * h.units[1]) * j / h.groups;
-  const int64_t u = (cost + kWideCost - 1) / kWideCost;
-  return u < h.units[0] ? u : h.units[0];
-}
-__host__ __device__ inline int64_t group_narrow_begin(const AttendHead& h, int64_t j) {
-  const int64_t wide = kWideCost * h.units[0], cost = (wide + kNarrowCost * h.units[1]) * j / h.groups;
-  const int64_t u = cost <= wide ? 0 : (cost - wide + kNarrowCost - 1) / kNarrowCost;
-  return u < h.units[1] ? u : h.units[1];
-}
-__host__ __device__ inline int64_t narrow_begin(const AttendHead& h, int64_t x) {
-  const int64_t j = x / kWavesPerGroup, a = group_narrow_begin(h, j);
-  return a + (group_narrow_begin(h, j + 1) - a) * (x % kWavesPerGroup) / kWavesPerGroup;
-}
-__host__ __device__ inline int64_t run_begin(const AttendHead& h, int kind, int64_t j) {
-  return kind == 0 ? wide_begin(h, j) : narrow_begin(h, j);
-}
-__host__ __device__ inline int32_t runs_of(const AttendHead& h, int kind) {
-  return kind == 0 ? h.groups : h.groups * kWavesPerGroup;
-}
-
-// Where a workgroup's or wave's run begins and ends.
+// Units that a workgroup (after its rounds) or a wave takes.
 struct alignas(16) AttendRun {
   int32_t tile, from;  // first tile, the first unit of it
-  int32_t units;       // in all; 0: nothing to do
-  int32_t number;      // among those of the head that have something to do
+  int32_t units;       // in all; 0: none
+  int32_t number;      // of the runs of its kind that have units
 };
 
 struct AttendPlanDev {
@@ -194,7 +175,8 @@ struct AttendPlanDev {
   AttendSeg* segs;    // 2 per place: prefix (first members only), own
   AttendTile* tiles[2];
   int64_t* begin[2];  // first unit of each tile
-  AttendRun* runs[2];  // of each workgroup of a head; of each wave, wave by wave of all workgroups
+  AttendRun* runs[2];
+  int64_t* run_at[2];  // first unit of each run
   AttendJoin* joins;
   float* part;        // partial results: [head][slot rows][dim], weights as numerators
   float2* part_ml;    // their maxima (times scale * log2 e) and sums

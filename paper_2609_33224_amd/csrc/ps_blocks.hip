@@ -139,6 +139,7 @@ hipError_t each_buffer(ps_attend_plan* p, F f) {
     one(d.tiles[k], d.tile_cap[k]);
     one(d.begin[k], d.tile_cap[k]);
     one(d.runs[k], (size_t)d.groups * (k == 0 ? 1 : kWavesPerGroup));
+    one(d.run_at[k], (size_t)d.groups * (k == 0 ? 1 : kWavesPerGroup));
   }
   // (a row with partial results each, or a place of empty rows: twice where two tiles have some)
   one(d.joins, (size_t)d.slot_rows + rows + d.tile_cap[0]);
@@ -164,7 +165,7 @@ void size_plan(ps_attend_plan* p, int32_t num_cus) {
   // a wide tile is full but for the last one of each segment, and a row lies in two segments at most
   d.tile_cap[0] = (int32_t)(2 * n + 2 * rows / kWideRows + 1);
   d.tile_cap[1] = (int32_t)(2 * n + 1);
-  d.groups = std::max(1, num_cus * ps_attend_per_cu(p->dim) / p->kv_heads);
+  d.groups = std::max(2, num_cus * ps_attend_per_cu(p->dim) / p->kv_heads);  // (of both kinds one at least)
   // Of partial results: each row of a shared segment once, in both of its segments;
   // and the pieces of tiles that are cut, of which there are fewer than twice
   // as many as workgroups or waves that take them.
