@@ -456,7 +456,10 @@ __device__ inline int kswz(int row, int chunk) {
 // Positions of a wide step: 64, or 32 where a row's registers leave no room.
 constexpr int wide_positions(int DP) { return DP <= 128 ? 64 : 32; }
 
-template <bool kF16, bool kQ8, int DP>
+// kSplit = 1: each wave has 32 of the 128 rows and all positions of a step; 2: 32 of 64
+// rows and half of the positions, the halves' results joined at the end, so that
+// tiles of 64 rows keep all four SIMDs at work.
+template <bool kF16, bool kQ8, int DP, int kSplit>
 __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* smem, int32_t* odd_at) {
   constexpr int kSteps = DP / 16;
   constexpr int kTok = wide_positions(DP);
@@ -464,11 +467,13 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
   constexpr int kLoads = (kQ8 ? DP / 16 : DP / 8) / kPer;  // 16-byte loads per thread
   constexpr int kDB = DP / 32;
   constexpr int kTile = kTok * DP * 2;
+  constexpr int kMine = kTok / kSplit;  // positions of a step that are the wave's
   const int lane = fresh(threadIdx.x & 63), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, hb = lane >> 5;
   const int D = a.cache.dim;
-  const int32_t r = wave * 32 + col;
-  const bool idle = wave * 32 >= p.rows;
+  const int rows0 = wave / kSplit * 32, off0 = wave % kSplit * kMine;
+  const int32_t r = rows0 + col;
+  const bool idle = rows0 >= p.rows;
 
   f32x16 acc[kDB];
 #pragma unroll
@@ -554,26 +559,26 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
       const unsigned char* ks = smem + buf * 2 * kTile;
       const unsigned char* vs = ks + kTile;
       // scores: position 32 b + 8 (i / 4) + 4 hb + i % 4 of the tile's
-      f32x16 s[kTok / 32];
+      f32x16 s[kMine / 32];
 #pragma unroll
-      for (int b = 0; b < kTok / 32; ++b) {
+      for (int b = 0; b < kMine / 32; ++b) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[b][i] = 0;
 #pragma unroll
         for (int st = 0; st < kSteps; ++st)
-          s[b] = mfma32<kF16>(*(const u32x4*)(ks + kswz<DP>(32 * b + col, 2 * st + hb)), q[st], s[b]);
+          s[b] = mfma32<kF16>(*(const u32x4*)(ks + kswz<DP>(off0 + 32 * b + col, 2 * st + hb)), q[st], s[b]);
       }
       const bool masked = t + kTok > p.tb || t + kTok > least;
       if (masked) {
 #pragma unroll
-        for (int b = 0; b < kTok / 32; ++b)
+        for (int b = 0; b < kMine / 32; ++b)
 #pragma unroll
           for (int i = 0; i < 16; ++i)
-            if (t + 32 * b + 8 * (i >> 2) + 4 * hb + (i & 3) >= min(lim, p.tb)) s[b][i] = -INFINITY;
+            if (t + off0 + 32 * b + 8 * (i >> 2) + 4 * hb + (i & 3) >= min(lim, p.tb)) s[b][i] = -INFINITY;
       }
       float top = s[0][0];
 #pragma unroll
-      for (int i = 1; i < kTok / 2; ++i) top = fmaxf(top, s[i >> 4][i & 15]);
+      for (int i = 1; i < kMine / 2; ++i) top = fmaxf(top, s[i >> 4][i & 15]);
       top = fmaxf(top, __shfl_xor(top, 32, 64));
       const float nm = fmaxf(m, top), mc = nm == -INFINITY ? 0.0f : nm * p.c;
       if (__any(nm > m)) {  // (a factor of 1 otherwise)
@@ -583,10 +588,10 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
         for (int k = 0; k < kDB; ++k) acc[k] *= f;
       }
       m = nm;
-      u32x4 pr[kTok / 16];
+      u32x4 pr[kMine / 16];
       float sum = 0;
 #pragma unroll
-      for (int x = 0; x < kTok / 16; ++x)
+      for (int x = 0; x < kMine / 16; ++x)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int at = (x & 1) * 8 + 2 * i;
@@ -599,14 +604,14 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
       // lane: element 32 k + col; positions 16 x + 8 jj + 4 hb ..
       auto turned = [&](int x, int k) {
         const int i = lane & 15, sub = (lane >> 4) & 1;
-        const int row = 16 * x + 4 * hb + (i >> 2), ch = 4 * k + 2 * sub + ((i & 2) >> 1), off = 8 * (i & 1);
+        const int row = off0 + 16 * x + 4 * hb + (i >> 2), ch = 4 * k + 2 * sub + ((i & 2) >> 1), off = 8 * (i & 1);
         const u32x2 y0 = read_turned(vs + vswz<DP>(row, ch) + off);
         const u32x2 y1 = read_turned(vs + vswz<DP>(row + 8, ch) + off);
         return u32x4{y0[0], y0[1], y1[0], y1[1]};
       };
       if (masked && odd_at[buf] == t)
 #pragma unroll 1
-        for (int32_t o = t; o < min(t + kTok, p.tb); ++o)
+        for (int32_t o = t + off0; o < min(t + off0 + kMine, p.tb); ++o)
 #pragma unroll
           for (int k = 0; k < 4 * kDB; ++k) {
             const f32x4 x = odd_values<kF16, kQ8>(a, p, o, min(8 * k + fresh(4 * hb), D - 4));
@@ -614,7 +619,7 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
             for (int i = 0; i < 4; ++i) acc[k >> 2][4 * (k & 3) + i] += o < lim ? x[i] : 0.0f;
           }
 #pragma unroll
-      for (int x = 0; x < kTok / 16; ++x)
+      for (int x = 0; x < kMine / 16; ++x)
 #pragma unroll
         for (int k = 0; k < kDB; ++k) acc[k] = mfma32<kF16>(turned(x, k), pr[x], acc[k]);
     }
@@ -622,8 +627,41 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
     __syncthreads();
   }
   l += __shfl_xor(l, 32, 64);
+  if (kSplit == 2) {
+    // the second half's results to the first half's wave
+    float2* ml = (float2*)(smem + 2 * 32 * DP * 4);
+    f32x4* os = (f32x4*)(smem + (wave >> 1) * 32 * DP * 4);
+    if (wave & 1) {
+      if (hb == 0) ml[r] = float2{m, l};
+#pragma unroll
+      for (int k = 0; k < kDB; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          os[(4 * k + i) * 64 + lane] =
+              f32x4{acc[k][4 * i], acc[k][4 * i + 1], acc[k][4 * i + 2], acc[k][4 * i + 3]};
+    }
+    __syncthreads();
+    if (!(wave & 1)) {
+      const float2 x = ml[r];
+      const float top = fmaxf(m, x.x), mc = top == -INFINITY ? 0.0f : top * p.c;
+      const float f = __builtin_amdgcn_exp2f(__builtin_fmaf(m, p.c, -mc));
+      const float fx = __builtin_amdgcn_exp2f(__builtin_fmaf(x.x, p.c, -mc));
+      l = l * f + x.y * fx;
+      m = top;
+#pragma unroll
+      for (int k = 0; k < kDB; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const f32x4 o = os[(4 * k + i) * 64 + lane];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[k][4 * i + e] = acc[k][4 * i + e] * f + o[e] * fx;
+        }
+    }
+    __syncthreads();
+    if (wave & 1) return;
+  }
   const int at = fresh(lane), d0 = 4 * (at >> 5);
-  const int32_t ro = wave * 32 + (at & 31);
+  const int32_t ro = rows0 + (at & 31);
   if (ro < p.rows) {
     const float inv = put_ml(a, p, ro, m, l, d0 == 0);
 #pragma unroll
@@ -687,7 +725,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_kernel(AttendAr
     p.ta = t0 + from * kUnit;
     p.tb = min(t1, t0 + (from + n) * kUnit);
     p.slot = slot < 0 ? -1 : slot + (piece - uniform(t.first)) * p.rows;
-    if (kind == 0) wide_piece<kF16, kQ8, DP>(a, p, smem, odd_at);
+    if (kind == 0 && DP <= 128 && p.rows <= 64) wide_piece<kF16, kQ8, DP, DP <= 128 ? 2 : 1>(a, p, smem, odd_at);
+    else if (kind == 0) wide_piece<kF16, kQ8, DP, 1>(a, p, smem, odd_at);
     else narrow_piece<kF16, kQ8, DP, kNarrowRows / 16>(a, p, smem + wave * narrow_positions(kQ8, DP) * DP * 2);
     if (most != INT32_MAX) left -= n;
   }

@@ -274,7 +274,10 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
         [&](int32_t k, int64_t at) { p.begin[kind][k] = at; });
   }
   {
-    const int64_t wide = kWideCost * units[0], all = wide + kNarrowCost * units[1];
+    int64_t mine = 0, wide;
+    for (int32_t k = tid; k < n_tiles[0]; k += kThreads) mine += units_of(p.tiles[0][k]) * (kUnitCost + p.tiles[0][k].rows);
+    block_scan(mine, &wide, sums);
+    const int64_t all = wide + kUnitCost * units[1];
     int64_t n_wide = all > 0 ? (wide * p.groups + all / 2) / all : 0;
     if (units[0] > 0) n_wide = max(n_wide, (int64_t)1);
     if (units[1] > 0) n_wide = min(n_wide, (int64_t)p.groups - 1);

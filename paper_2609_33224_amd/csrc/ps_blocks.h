@@ -106,9 +106,9 @@ constexpr int kUnit = 64;
 constexpr int kWideRows = 128;
 constexpr int kNarrowRows = 16;
 constexpr int kWavesPerGroup = 4;
-// Cost of a unit for a workgroup: 2.9 us of a wide tile's, 1.5 (8 bits) to 3.0 us (16
-// bits) of a narrow one's, with every workgroup at work.
-constexpr int kWideCost = 3, kNarrowCost = 2;
+// Cost of a unit for a workgroup, in rows: of a narrow tile's (1.5 to 1.75 us of e4m3
+// with every workgroup at work), and what a wide one's has beside its rows (3.7 us for 128).
+constexpr int kUnitCost = 128;
 constexpr int kShareMinTokens = 64;  // of a prefix
 constexpr int kShareMaxRows = 64;    // of a member (or one row of all its heads)
 
