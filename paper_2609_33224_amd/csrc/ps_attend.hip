@@ -132,19 +132,21 @@ __device__ inline int32_t block_of(const AttendArgs& a, int32_t t) {
   return (int32_t)((__umulhi((uint32_t)t, a.bt_mul) + (uint32_t)t) >> a.bt_shift);
 }
 
-// The page of position t.  (Its number was checked when the plan was made; one that
-// has changed since is kept inside the cache.)
+// The page of position t, as it is read: nothing is computed from it here, since
+// that would wait for it, and for every load before it.
 __device__ inline uint32_t page_of(const AttendArgs& a, const Chain& c, int32_t t) {
   const int32_t b = block_of(a, t);
-  const uint32_t page = (uint32_t)c.pages[b < c.pre_len ? c.pre_off + b : c.tail_off + (b - c.pre_len)];
-  return min(page, (uint32_t)a.cache.n_pages - 1u);
+  return (uint32_t)c.pages[b < c.pre_len ? c.pre_off + b : c.tail_off + (b - c.pre_len)];
 }
 
 struct Spot {
   int64_t at;  // first element of the row
   int64_t x;   // its exponent
 };
+// (A page number was checked when the plan was made; one that has changed since is
+// kept inside the cache.)
 __device__ inline Spot spot_of(const AttendArgs& a, int32_t head, uint32_t page, int32_t t) {
+  page = min(page, (uint32_t)a.cache.n_pages - 1u);
   const int32_t slot = t - block_of(a, t) * a.win.bt;
   const int32_t r = head * a.win.bt + slot;
   return Spot{(int64_t)page * a.cache.page_stride + (int64_t)r * a.cache.dim, (int64_t)page * a.cache.exp_stride + r};
@@ -231,13 +233,13 @@ __device__ inline float put_ml(const AttendArgs& a, const Piece& p, int32_t r, f
 
 // ------------------------------------------------------------------ narrow
 
-// Shared memory of a wave's 32 positions of values: DP elements a row, chunks
-// of 8 at chunk ^ 2 (row % 8), so that neither the rows' writes nor the turned reads
-// of 16 rows meet in a bank more than their size makes them.
-template <int DP>
-__device__ inline int vswz(int row, int chunk) {
-  return row * (DP * 2) + ((chunk ^ ((row & 7) << 1)) & (DP / 8 - 1)) * 16;
-}
+// Rows of values in shared memory, in bytes: padded so that the turned reads of 16
+// rows (narrow: 32 bytes each) or 8 rows (wide: 64 bytes each) take every bank the
+// same number of times; rows of keys so that 8 of them differ in their banks.  Padding
+// rather than swizzled chunks: all offsets are then constants of the instructions.
+constexpr int narrow_stride(int DP) { return DP * 2 + 32; }
+constexpr int value_stride(int DP) { return DP * 2 + 64; }
+constexpr int key_stride(int DP) { return DP * 2 + 16; }
 
 // Positions of a narrow step: enough that a wave has 16 KB of a head of 128 in flight.
 constexpr int narrow_positions(bool kQ8, int DP) { return kQ8 && DP <= 128 ? 64 : 32; }
@@ -250,6 +252,7 @@ __device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char*
   constexpr int kSteps = DP / 32;                     // of the first product
   constexpr int kLoads = kQ8 ? DP / 64 : DP / 32;     // 16-byte loads per lane and 16 positions
   constexpr int kDB = DP / 16;                        // blocks of the second product
+  constexpr int kV = narrow_stride(DP);
   const int lane = fresh(threadIdx.x & 63), col = lane & 15, g = lane >> 4;
   const int D = a.cache.dim;
 
@@ -335,11 +338,11 @@ __device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char*
             odd |= clean8<kF16>(x);
             odd |= clean8<kF16>(y);
           }
-          *(u32x4*)(vs + vswz<DP>(row, 8 * i + 2 * g)) = x;
-          *(u32x4*)(vs + vswz<DP>(row, 8 * i + 2 * g + 1)) = y;
+          *(u32x4*)(vs + row * kV + (8 * i + 2 * g) * 16) = x;
+          *(u32x4*)(vs + row * kV + (8 * i + 2 * g + 1) * 16) = y;
         } else {
           if (masked) odd |= clean8<kF16>(vr[h][i]);
-          *(u32x4*)(vs + vswz<DP>(row, 4 * i + g)) = vr[h][i];
+          *(u32x4*)(vs + row * kV + (4 * i + g) * 16) = vr[h][i];
         }
       }
     // scores: position 16 h + 4 g + i of the step, row b * 16 + col
@@ -361,10 +364,10 @@ __device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char*
         for (int b = 0; b < RB; ++b) s[b][h] = mfma16<kF16>(ka, q[b][st], s[b][h]);
       }
     }
-    if (t + kTok < p.tb) {
-      loads(t + kTok);
-      pages(t + 2 * kTok);
-    }
+    // (behind the last step too, its last position over: of loads that depend on a branch
+    // the registers are copied behind it, which waits for them)
+    loads(t + kTok);
+    pages(t + 2 * kTok);
     // (the rows that other lanes wrote)
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 
@@ -405,9 +408,9 @@ __device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char*
     }
     // lane i of 16: row 4 g + i / 4, elements 16 k + 4 (i % 4) ..
     auto turned = [&](int x, int k) {
-      const int row = 32 * x + 4 * g + (col >> 2), half = (col & 2) >> 1, off = 8 * (col & 1);
-      const u32x2 y0 = read_turned(vs + vswz<DP>(row, 2 * k + half) + off);
-      const u32x2 y1 = read_turned(vs + vswz<DP>(16 + row, 2 * k + half) + off);
+      const unsigned char* at = vs + (4 * g + (col >> 2)) * kV + (col & 3) * 8;
+      const u32x2 y0 = read_turned(at + 32 * x * kV + 32 * k);
+      const u32x2 y1 = read_turned(at + (32 * x + 16) * kV + 32 * k);
       return u32x4{y0[0], y0[1], y1[0], y1[1]};
     };
     if (masked && __any(odd != 0))
@@ -448,11 +451,6 @@ __device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char*
 
 // ------------------------------------------------------------------ wide
 
-template <int DP>
-__device__ inline int kswz(int row, int chunk) {
-  return row * (DP * 2) + ((chunk ^ row) & (DP / 8 - 1)) * 16;
-}
-
 // Positions of a wide step: 64, or 32 where a row's registers leave no room.
 constexpr int wide_positions(int DP) { return DP <= 128 ? 64 : 32; }
 
@@ -466,7 +464,8 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
   constexpr int kPer = 256 / kTok;                               // threads that stage a row
   constexpr int kLoads = (kQ8 ? DP / 16 : DP / 8) / kPer;  // 16-byte loads per thread
   constexpr int kDB = DP / 32;
-  constexpr int kTile = kTok * DP * 2;
+  constexpr int kK = key_stride(DP), kV = value_stride(DP);
+  constexpr int kKeys = kTok * kK, kTile = kTok * (kK + kV);  // bytes of a step's keys; of all
   constexpr int kMine = kTok / kSplit;  // positions of a step that are the wave's
   const int lane = fresh(threadIdx.x & 63), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, hb = lane >> 5;
@@ -508,26 +507,26 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
   auto stage = [&](int buf, int32_t t) {
     const bool masked = t + kTok > p.tb || t + kTok > least_of_all;
     uint32_t odd = 0;
-    unsigned char* ks = smem + buf * 2 * kTile;
-    unsigned char* vs = ks + kTile;
+    unsigned char* ks = smem + buf * kTile + srow * kK + sc * (kQ8 ? 32 : 16);
+    unsigned char* vs = smem + buf * kTile + kKeys + srow * kV + sc * (kQ8 ? 32 : 16);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
+      const int off = kPer * (kQ8 ? 32 : 16) * i;
       if (kQ8) {
         const float sk = scale_of(kx), sv = scale_of(vx);
-        const int ch = 2 * (kPer * i + sc);
-        *(u32x4*)(ks + kswz<DP>(srow, ch)) = widen8<kF16>(kr[i][0], kr[i][1], sk);
-        *(u32x4*)(ks + kswz<DP>(srow, ch + 1)) = widen8<kF16>(kr[i][2], kr[i][3], sk);
+        *(u32x4*)(ks + off) = widen8<kF16>(kr[i][0], kr[i][1], sk);
+        *(u32x4*)(ks + off + 16) = widen8<kF16>(kr[i][2], kr[i][3], sk);
         u32x4 x = widen8<kF16>(vr[i][0], vr[i][1], sv), y = widen8<kF16>(vr[i][2], vr[i][3], sv);
         if (masked) {  // (as in the narrow kernel)
           odd |= clean8<kF16>(x);
           odd |= clean8<kF16>(y);
         }
-        *(u32x4*)(vs + vswz<DP>(srow, ch)) = x;
-        *(u32x4*)(vs + vswz<DP>(srow, ch + 1)) = y;
+        *(u32x4*)(vs + off) = x;
+        *(u32x4*)(vs + off + 16) = y;
       } else {
         if (masked) odd |= clean8<kF16>(vr[i]);
-        *(u32x4*)(ks + kswz<DP>(srow, kPer * i + sc)) = kr[i];
-        *(u32x4*)(vs + vswz<DP>(srow, kPer * i + sc)) = vr[i];
+        *(u32x4*)(ks + off) = kr[i];
+        *(u32x4*)(vs + off) = vr[i];
       }
     }
     if (odd) odd_at[buf] = t;  // (a value left by another piece only costs a look)
@@ -550,14 +549,12 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
   __syncthreads();
   int buf = 0;
   for (int32_t t = p.ta; t < p.tb; t += kTok, buf ^= 1) {
-    const bool more = t + kTok < p.tb;
-    if (more) {
-      loads(t + kTok);
-      pages(t + 2 * kTok);
-    }
+    loads(t + kTok);  // (behind the last step too: as in the narrow kernel)
+    pages(t + 2 * kTok);
     if (!idle) {
-      const unsigned char* ks = smem + buf * 2 * kTile;
-      const unsigned char* vs = ks + kTile;
+      const unsigned char* ks = smem + buf * kTile + (off0 + col) * kK + hb * 16;
+      const unsigned char* vs =
+          smem + buf * kTile + kKeys + (off0 + 4 * hb + ((lane & 15) >> 2)) * kV + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
       // scores: position 32 b + 8 (i / 4) + 4 hb + i % 4 of the tile's
       f32x16 s[kMine / 32];
 #pragma unroll
@@ -566,7 +563,7 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
         for (int i = 0; i < 16; ++i) s[b][i] = 0;
 #pragma unroll
         for (int st = 0; st < kSteps; ++st)
-          s[b] = mfma32<kF16>(*(const u32x4*)(ks + kswz<DP>(off0 + 32 * b + col, 2 * st + hb)), q[st], s[b]);
+          s[b] = mfma32<kF16>(*(const u32x4*)(ks + 32 * b * kK + 32 * st), q[st], s[b]);
       }
       const bool masked = t + kTok > p.tb || t + kTok > least;
       if (masked) {
@@ -603,10 +600,8 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
       l += sum;
       // lane: element 32 k + col; positions 16 x + 8 jj + 4 hb ..
       auto turned = [&](int x, int k) {
-        const int i = lane & 15, sub = (lane >> 4) & 1;
-        const int row = off0 + 16 * x + 4 * hb + (i >> 2), ch = 4 * k + 2 * sub + ((i & 2) >> 1), off = 8 * (i & 1);
-        const u32x2 y0 = read_turned(vs + vswz<DP>(row, ch) + off);
-        const u32x2 y1 = read_turned(vs + vswz<DP>(row + 8, ch) + off);
+        const u32x2 y0 = read_turned(vs + 16 * x * kV + 64 * k);
+        const u32x2 y1 = read_turned(vs + (16 * x + 8) * kV + 64 * k);
         return u32x4{y0[0], y0[1], y1[0], y1[1]};
       };
       if (masked && odd_at[buf] == t)
@@ -623,7 +618,7 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
 #pragma unroll
         for (int k = 0; k < kDB; ++k) acc[k] = mfma32<kF16>(turned(x, k), pr[x], acc[k]);
     }
-    if (more) stage(buf ^ 1, t + kTok);
+    if (t + kTok < p.tb) stage(buf ^ 1, t + kTok);
     __syncthreads();
   }
   l += __shfl_xor(l, 32, 64);
@@ -673,9 +668,15 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
   }
 }
 
+constexpr int shared_bytes(bool kQ8, int DP) {
+  const int wide = 2 * wide_positions(DP) * (key_stride(DP) + value_stride(DP));
+  const int narrow = kWavesPerGroup * narrow_positions(kQ8, DP) * narrow_stride(DP);
+  return wide > narrow ? wide : narrow;
+}
+
 template <bool kF16, bool kQ8, int DP>
 __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_kernel(AttendArgs a) {
-  __shared__ __align__(16) unsigned char smem[4 * wide_positions(DP) * DP * 2];
+  __shared__ __align__(16) unsigned char smem[shared_bytes(kQ8, DP)];
   __shared__ int32_t odd_at[2];
   if (threadIdx.x < 2) odd_at[threadIdx.x] = -1;
   __syncthreads();
@@ -727,7 +728,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_kernel(AttendAr
     p.slot = slot < 0 ? -1 : slot + (piece - uniform(t.first)) * p.rows;
     if (kind == 0 && DP <= 128 && p.rows <= 64) wide_piece<kF16, kQ8, DP, DP <= 128 ? 2 : 1>(a, p, smem, odd_at);
     else if (kind == 0) wide_piece<kF16, kQ8, DP, 1>(a, p, smem, odd_at);
-    else narrow_piece<kF16, kQ8, DP, kNarrowRows / 16>(a, p, smem + wave * narrow_positions(kQ8, DP) * DP * 2);
+    else narrow_piece<kF16, kQ8, DP, kNarrowRows / 16>(a, p, smem + wave * narrow_positions(kQ8, DP) * narrow_stride(DP));
     if (most != INT32_MAX) left -= n;
   }
 }
