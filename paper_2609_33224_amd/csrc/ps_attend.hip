@@ -106,6 +106,13 @@ __device__ inline int fresh(int x) {
   return x;
 }
 
+// x + y, done here: a rare loop's sums are not put off until all of its loads are in registers.
+__device__ inline float added(float x, float y) {
+  x += y;
+  asm volatile("" : "+v"(x) : : "memory");
+  return x;
+}
+
 // Four rows' elements to a lane each: of 16 lanes that point to 4 rows of 16
 // elements (4 lanes a row, 4 elements a lane), lane i receives column i.
 __device__ inline u32x2 read_turned(const unsigned char* p) {
@@ -123,8 +130,8 @@ __device__ inline int64_t uniform(int64_t x) {
 
 // The chain of a tile, with what it takes to find a position's bytes.
 struct Chain {
-  const int32_t* pages;
-  int64_t pre_off, tail_off;
+  const int32_t* pre;   // the page of block 0 of the prefix segment
+  const int32_t* tail;  // the page of the tail's first block, less pre_len
   int32_t pre_len;
 };
 
@@ -136,7 +143,7 @@ __device__ inline int32_t block_of(const AttendArgs& a, int32_t t) {
 // that would wait for it, and for every load before it.
 __device__ inline uint32_t page_of(const AttendArgs& a, const Chain& c, int32_t t) {
   const int32_t b = block_of(a, t);
-  return (uint32_t)c.pages[b < c.pre_len ? c.pre_off + b : c.tail_off + (b - c.pre_len)];
+  return (uint32_t)(b < c.pre_len ? c.pre : c.tail)[b];
 }
 
 struct Spot {
@@ -380,7 +387,7 @@ __device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char*
           for (int i = 0; i < 4; ++i)
             if (t + 16 * h + 4 * g + i >= min(lim[b], p.tb)) s[b][h][i] = -INFINITY;
     }
-    u32x4 pr[RB][kX];
+    float mc[RB];
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
       float top = s[b][0][0];
@@ -388,31 +395,14 @@ __device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char*
       for (int i = 1; i < 4 * kH; ++i) top = fmaxf(top, s[b][i >> 2][i & 3]);
       top = fmaxf(top, __shfl_xor(top, 16, 64));
       top = fmaxf(top, __shfl_xor(top, 32, 64));
-      const float nm = fmaxf(m[b], top), mc = nm == -INFINITY ? 0.0f : nm * p.c;
-      const float f = __builtin_amdgcn_exp2f(__builtin_fmaf(m[b], p.c, -mc));
+      const float nm = fmaxf(m[b], top);
+      mc[b] = nm == -INFINITY ? 0.0f : nm * p.c;
+      const float f = __builtin_amdgcn_exp2f(__builtin_fmaf(m[b], p.c, -mc[b]));
       m[b] = nm;
-      float sum = 0;
-#pragma unroll
-      for (int x = 0; x < kX; ++x)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const f32x4& v = s[b][2 * x + (i >> 1)];
-          const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(v[(2 * i) & 3], p.c, -mc));
-          const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(v[(2 * i + 1) & 3], p.c, -mc));
-          sum += e0 + e1;
-          pr[b][x][i] = pack<kF16>(e0, e1);
-        }
-      l[b] = __builtin_fmaf(l[b], f, sum);
+      l[b] *= f;
 #pragma unroll
       for (int k = 0; k < kDB; ++k) acc[b][k] *= f;
     }
-    // lane i of 16: row 4 g + i / 4, elements 16 k + 4 (i % 4) ..
-    auto turned = [&](int x, int k) {
-      const unsigned char* at = vs + (4 * g + (col >> 2)) * kV + (col & 3) * 8;
-      const u32x2 y0 = read_turned(at + 32 * x * kV + 32 * k);
-      const u32x2 y1 = read_turned(at + (32 * x + 16) * kV + 32 * k);
-      return u32x4{y0[0], y0[1], y1[0], y1[1]};
-    };
     if (masked && __any(odd != 0))
 #pragma unroll 1
       for (int32_t o = t; o < min(t + kTok, p.tb); ++o)
@@ -422,16 +412,38 @@ __device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char*
 #pragma unroll
           for (int b = 0; b < RB; ++b)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) acc[b][k][i] += o < lim[b] ? x[i] : 0.0f;
+            for (int i = 0; i < 4; ++i) acc[b][k][i] = added(acc[b][k][i], o < lim[b] ? x[i] : 0.0f);
         }
+    // lane i of 16: row 4 g + i / 4, elements 16 k + 4 (i % 4) ..
+    auto turned = [&](int x, int k) {
+      const unsigned char* at = vs + (4 * g + (col >> 2)) * kV + (col & 3) * 8;
+      const u32x2 y0 = read_turned(at + 32 * x * kV + 32 * k);
+      const u32x2 y1 = read_turned(at + (32 * x + 16) * kV + 32 * k);
+      return u32x4{y0[0], y0[1], y1[0], y1[1]};
+    };
 #pragma unroll
-    for (int x = 0; x < kX; ++x)
+    for (int x = 0; x < kX; ++x) {
+      u32x4 va[kDB], pr[RB];
+#pragma unroll
+      for (int k = 0; DP <= 128 && k < kDB; ++k) va[k] = turned(x, k);
+#pragma unroll
+      for (int b = 0; b < RB; ++b) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const f32x4& v = s[b][2 * x + (i >> 1)];
+          const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(v[(2 * i) & 3], p.c, -mc[b]));
+          const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(v[(2 * i + 1) & 3], p.c, -mc[b]));
+          l[b] += e0 + e1;
+          pr[b][i] = pack<kF16>(e0, e1);
+        }
+      }
 #pragma unroll
       for (int k = 0; k < kDB; ++k) {
-        const u32x4 va = turned(x, k);
+        if (DP > 128) va[0] = turned(x, k);  // (no registers to read ahead)
 #pragma unroll
-        for (int b = 0; b < RB; ++b) acc[b][k] = mfma16<kF16>(va, pr[b][x], acc[b][k]);
+        for (int b = 0; b < RB; ++b) acc[b][k] = mfma16<kF16>(va[DP > 128 ? 0 : k], pr[b], acc[b][k]);
       }
+    }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
 
@@ -539,9 +551,15 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
   const int64_t qat = a.plan.row[qrow.place] * a.q.row + (int64_t)qrow.head * a.q.head;
   loads(p.ta);
   pages(p.ta + kTok);
-  u32x4 q[kSteps];
+  // (heads above 128: no registers for q, it stays in shared memory)
+  u32x4 q[DP <= 128 ? kSteps : 1];
+  unsigned char* qs = smem + 2 * kTile + (wave * 32 + col) * kK + hb * 16;
 #pragma unroll
-  for (int s = 0; s < kSteps; ++s) q[s] = load_q(a, p, qat, r < p.rows, 16 * s + 8 * hb);
+  for (int s = 0; s < kSteps; ++s) {
+    const u32x4 x = load_q(a, p, qat, r < p.rows, 16 * s + 8 * hb);
+    if (DP <= 128) q[s] = x;
+    else *(u32x4*)(qs + 32 * s) = x;
+  }
   if (r >= p.rows) lim = INT32_MAX;
   int32_t least = lim;
   for (int o = 16; o > 0; o >>= 1) least = min(least, __shfl_xor(least, o, 64));
@@ -563,7 +581,8 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
         for (int i = 0; i < 16; ++i) s[b][i] = 0;
 #pragma unroll
         for (int st = 0; st < kSteps; ++st)
-          s[b] = mfma32<kF16>(*(const u32x4*)(ks + 32 * b * kK + 32 * st), q[st], s[b]);
+          s[b] = mfma32<kF16>(*(const u32x4*)(ks + 32 * b * kK + 32 * st),
+                              DP <= 128 ? q[DP <= 128 ? st : 0] : *(const u32x4*)(qs + 32 * st), s[b]);
       }
       const bool masked = t + kTok > p.tb || t + kTok > least;
       if (masked) {
@@ -585,10 +604,31 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
         for (int k = 0; k < kDB; ++k) acc[k] *= f;
       }
       m = nm;
-      u32x4 pr[kMine / 16];
-      float sum = 0;
+      if (masked && odd_at[buf] == t)
+#pragma unroll 1
+        for (int32_t o = t + off0; o < min(t + off0 + kMine, p.tb); ++o)
 #pragma unroll
-      for (int x = 0; x < kMine / 16; ++x)
+          for (int k = 0; k < 4 * kDB; ++k) {
+            const f32x4 x = odd_values<kF16, kQ8>(a, p, o, min(8 * k + fresh(4 * hb), D - 4));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[k >> 2][4 * (k & 3) + i] = added(acc[k >> 2][4 * (k & 3) + i], o < lim ? x[i] : 0.0f);
+          }
+      // lane: element 32 k + col; positions 16 x + 8 jj + 4 hb ..
+      auto turned = [&](int x, int k) {
+        const u32x2 y0 = read_turned(vs + 16 * x * kV + 64 * k);
+        const u32x2 y1 = read_turned(vs + (16 * x + 8) * kV + 64 * k);
+        return u32x4{y0[0], y0[1], y1[0], y1[1]};
+      };
+      // 16 positions at a time: the products of the ones before run beside the
+      // exponentials of these.  (Heads above 128: no registers for that.)
+      float sum = 0;
+      u32x4 pr[kMine / 16];
+#pragma unroll
+      for (int x = 0; x < kMine / 16; ++x) {
+        u32x4 va[kDB];
+        if (DP <= 128)
+#pragma unroll
+          for (int k = 0; k < kDB; ++k) va[k] = turned(x, k);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int at = (x & 1) * 8 + 2 * i;
@@ -597,26 +637,16 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
           sum += e0 + e1;
           pr[x][i] = pack<kF16>(e0, e1);
         }
+        if (DP <= 128)
+#pragma unroll
+          for (int k = 0; k < kDB; ++k) acc[k] = mfma32<kF16>(va[k], pr[x], acc[k]);
+      }
+      if (DP > 128)
+#pragma unroll
+        for (int x = 0; x < kMine / 16; ++x)
+#pragma unroll
+          for (int k = 0; k < kDB; ++k) acc[k] = mfma32<kF16>(turned(x, k), pr[x], acc[k]);
       l += sum;
-      // lane: element 32 k + col; positions 16 x + 8 jj + 4 hb ..
-      auto turned = [&](int x, int k) {
-        const u32x2 y0 = read_turned(vs + 16 * x * kV + 64 * k);
-        const u32x2 y1 = read_turned(vs + (16 * x + 8) * kV + 64 * k);
-        return u32x4{y0[0], y0[1], y1[0], y1[1]};
-      };
-      if (masked && odd_at[buf] == t)
-#pragma unroll 1
-        for (int32_t o = t + off0; o < min(t + off0 + kMine, p.tb); ++o)
-#pragma unroll
-          for (int k = 0; k < 4 * kDB; ++k) {
-            const f32x4 x = odd_values<kF16, kQ8>(a, p, o, min(8 * k + fresh(4 * hb), D - 4));
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[k >> 2][4 * (k & 3) + i] += o < lim ? x[i] : 0.0f;
-          }
-#pragma unroll
-      for (int x = 0; x < kMine / 16; ++x)
-#pragma unroll
-        for (int k = 0; k < kDB; ++k) acc[k] = mfma32<kF16>(turned(x, k), pr[x], acc[k]);
     }
     if (t + kTok < p.tb) stage(buf ^ 1, t + kTok);
     __syncthreads();
@@ -669,7 +699,7 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
 }
 
 constexpr int shared_bytes(bool kQ8, int DP) {
-  const int wide = 2 * wide_positions(DP) * (key_stride(DP) + value_stride(DP));
+  const int wide = 2 * wide_positions(DP) * (key_stride(DP) + value_stride(DP)) + (DP > 128 ? kWideRows * key_stride(DP) : 0);
   const int narrow = kWavesPerGroup * narrow_positions(kQ8, DP) * narrow_stride(DP);
   return wide > narrow ? wide : narrow;
 }
@@ -684,7 +714,6 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_kernel(AttendAr
   const int32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const float c = a.scale * 1.44269504088896341f;
   Piece p;
-  p.chain.pages = a.win.pages;
   p.head = head;
   p.c = fmaxf(fabsf(c), 1.17549435e-38f);  // (not 0: it multiplies infinities)
   p.neg = c < 0 ? 0x80008000u : 0u;
@@ -717,9 +746,9 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_kernel(AttendAr
     const int32_t t0 = uniform(t.t0), t1 = uniform(t.t1), slot = uniform(t.slot);
     const int32_t n = min(max(0, (t1 - t0 + kUnit - 1) / kUnit) - from, most);
     if (n <= 0) continue;  // (a tile of no positions)
-    p.chain.pre_off = uniform(t.pre_off);
-    p.chain.tail_off = uniform(t.tail_off);
     p.chain.pre_len = uniform(t.pre_len);
+    p.chain.pre = a.win.pages + uniform(t.pre_off);
+    p.chain.tail = a.win.pages + (uniform(t.tail_off) - p.chain.pre_len);
     p.p0 = uniform(t.p0);
     p.row0 = uniform(t.row0);
     p.rows = uniform(t.rows);

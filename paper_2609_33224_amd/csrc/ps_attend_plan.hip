@@ -4,6 +4,8 @@
 // then one workgroup cuts the work (thousands of small steps with a barrier
 // between; a step's layers share one plan).
 
+#include <type_traits>
+
 #include "ps_blocks.h"
 
 namespace ps {
@@ -31,18 +33,32 @@ __global__ __launch_bounds__(256) void plan_check_kernel(AttendPlanDev p, BlockW
   }
 }
 
+// Inclusive sums over the wave, by row shifts and row broadcasts.
+__device__ inline int64_t wave_scan(int64_t x) {
+  auto step = [&](auto shift, auto rows) {
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, shift(), rows(), 0xF, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(x >> 32), shift(), rows(), 0xF, false);
+    x += (int64_t)((uint64_t)hi << 32 | lo);
+  };
+  auto c = [](auto v) { return v; };
+  step(c(std::integral_constant<int, 0x111>{}), c(std::integral_constant<int, 0xF>{}));
+  step(c(std::integral_constant<int, 0x112>{}), c(std::integral_constant<int, 0xF>{}));
+  step(c(std::integral_constant<int, 0x114>{}), c(std::integral_constant<int, 0xF>{}));
+  step(c(std::integral_constant<int, 0x118>{}), c(std::integral_constant<int, 0xF>{}));
+  step(c(std::integral_constant<int, 0x142>{}), c(std::integral_constant<int, 0xA>{}));  // lanes 15, 47 to the next row
+  step(c(std::integral_constant<int, 0x143>{}), c(std::integral_constant<int, 0xC>{}));  // lane 31 to the upper half
+  return x;
+}
+
 // Exclusive sums over the workgroup of each thread's value; *total to all.
 __device__ inline int64_t block_scan(int64_t v, int64_t* total, int64_t* lds) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int64_t x = v;
-  for (int o = 1; o < 64; o <<= 1) {
-    const int64_t y = __shfl_up((long long)x, o, 64);
-    if (lane >= o) x += y;
-  }
+  const int64_t x = wave_scan(v);
   __syncthreads();
   if (lane == 63) lds[wave] = x;
   __syncthreads();
   int64_t before = 0, all = 0;
+#pragma unroll
   for (int i = 0; i < kWaves; ++i) {
     const int64_t y = lds[i];
     before += i < wave ? y : 0;
@@ -53,11 +69,23 @@ __device__ inline int64_t block_scan(int64_t v, int64_t* total, int64_t* lds) {
 }
 
 // Exclusive scan of value(i) for i in [0, n): store(i, sum before it); returns the sum.
+// One pass in rounds of a value per thread, or (many values) a run of them per thread.
 template <class V, class S>
 __device__ inline int64_t scan_all(int32_t n, int64_t* lds, V value, S store) {
+  int64_t total = 0;
+  if (n <= 4 * kThreads) {
+    int64_t before = 0;
+    for (int32_t i0 = 0; i0 < n; i0 += kThreads) {
+      const int32_t i = i0 + (int32_t)threadIdx.x;
+      const int64_t at = block_scan(i < n ? value(i) : 0, &total, lds);
+      if (i < n) store(i, before + at);
+      before += total;
+    }
+    return before;
+  }
   const int32_t per = (n + kThreads - 1) / kThreads;
   const int32_t a = min(n, per * (int32_t)threadIdx.x), b = min(n, a + per);
-  int64_t sum = 0, total;
+  int64_t sum = 0;
   for (int32_t i = a; i < b; ++i) sum += value(i);
   int64_t at = block_scan(sum, &total, lds);
   for (int32_t i = a; i < b; ++i) {
@@ -68,11 +96,42 @@ __device__ inline int64_t scan_all(int32_t n, int64_t* lds, V value, S store) {
   return total;
 }
 
+// The last of n ascending numbers that is at most u (the first one is).
+__device__ inline int32_t last_at_most(const int64_t* v, int32_t n, int64_t u) {
+  int32_t a = 0, b = n;
+  while (b - a > 1) {
+    const int32_t m = (a + b) >> 1;
+    if (v[m] <= u) a = m;
+    else b = m;
+  }
+  return a;
+}
+
+constexpr int kSmall = 1024;  // requests, up to which the tables lie in shared memory
+constexpr int kNear = 1024;   // tiles and runs of a kind, likewise
+
+__device__ inline int64_t units_of(const AttendTile& t) { return (max(0, t.t1 - t.t0) + kUnit - 1) / kUnit; }
+
+// The steps: groups of requests with one prefix; the order of requests (groups
+// together) and of their rows; segments; tiles; units and runs; partial results and
+// what is to be joined.  Each ends with a barrier, of which the kernel's time is made:
+// 13 us for one request, 21 us for 128 in 24 groups.
+template <bool kFits>
 __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, BlockWin w, int32_t ratio,
                                                             uint32_t* d_flags) {
-  __shared__ uint32_t keys[PS_MAX_WINDOW_REQ];
+  constexpr int kKeys = kFits ? kSmall : PS_MAX_WINDOW_REQ;
+  __shared__ uint32_t keys[kKeys];
+  __shared__ uint32_t unsorted[kFits ? kSmall : 1];
+  __shared__ int32_t near_table[kFits ? 2 * kSmall : 1], near_least[kFits ? 2 * kSmall : 1];
+  __shared__ int32_t near_slot[kFits ? kSmall : 1], near_members[kFits ? kSmall : 1], near_base[kFits ? kSmall : 1];
+  __shared__ int64_t near_begin[2][kNear], near_run[2][kNear];
   __shared__ int64_t sums[kWaves];
   __shared__ int32_t n_todo;
+  int32_t* const table = kFits ? near_table : p.table;
+  int32_t* const least = kFits ? near_least : p.least;
+  int32_t* const slot_of = kFits ? near_slot : p.slot_of;
+  int32_t* const members = kFits ? near_members : p.members;
+  int32_t* const base = kFits ? near_base : p.base;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int32_t n = w.n_req;
 
@@ -81,7 +140,13 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
   for (int32_t r = tid; r < n; r += kThreads) {
     const int32_t lo = w.row_off[r], hi = w.row_off[r + 1];
     bad |= lo < 0 || hi < lo || hi > w.n_rows;
+    members[r] = 0;
   }
+  for (int32_t i = tid; i <= p.table_mask; i += kThreads) {
+    table[i] = 0;
+    least[i] = INT32_MAX;
+  }
+  if (tid == 0) n_todo = 0;
   if (__syncthreads_or(bad)) {
     if (d_flags)
       for (int32_t r = tid; r < n; r += kThreads) d_flags[r] = PS_R_INVALID;
@@ -91,13 +156,6 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
 
   // Groups: requests with few rows, all of which see the whole prefix, meet
   // in a hash table by the place and length of their prefix.
-  for (int32_t i = tid; i <= p.table_mask; i += kThreads) {
-    p.table[i] = 0;
-    p.least[i] = INT32_MAX;
-  }
-  for (int32_t r = tid; r < n; r += kThreads) p.members[r] = 0;
-  if (tid == 0) n_todo = 0;
-  __syncthreads();
   for (int32_t r = tid; r < n; r += kThreads) {
     const BlockReq q = block_req(w, r);
     const int32_t rows = q.hi - q.lo;
@@ -108,85 +166,103 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
       uint64_t h = (uint64_t)q.pre_off * 0x9E3779B97F4A7C15ull ^ (uint64_t)q.pre_len * 0xC2B2AE3D27D4EB4Full;
       at = (int32_t)((h ^ h >> 32) & (uint32_t)p.table_mask);
       for (;;) {  // (at most half of the slots are taken)
-        const int32_t held = atomicCAS(&p.table[at], 0, r + 1);
+        const int32_t held = atomicCAS(&table[at], 0, r + 1);
         if (held == 0) break;
         const ps_req d = w.reqs[held - 1];
         if (d.pre_off == q.pre_off && d.pre_len == q.pre_len) break;
         at = (at + 1) & p.table_mask;
       }
-      atomicMin(&p.least[at], r);
+      atomicMin(&least[at], r);
     }
-    p.slot_of[r] = at;
+    slot_of[r] = at;
   }
   __syncthreads();
   for (int32_t r = tid; r < n; r += kThreads)
-    if (p.slot_of[r] >= 0) atomicAdd(&p.members[p.least[p.slot_of[r]]], 1);
+    if (slot_of[r] >= 0) atomicAdd(&members[least[slot_of[r]]], 1);
   __syncthreads();
 
   // The order: by the group's least member, then by request, whatever the
   // order in which the table was filled.
-  int32_t n2 = 64;
-  while (n2 < n) n2 <<= 1;
-  for (int32_t r = tid; r < n2; r += kThreads) {
-    uint32_t key = 0xFFFFFFFFu;
-    if (r < n) {
-      const int32_t at = p.slot_of[r];
-      const int32_t first = at >= 0 && p.members[p.least[at]] > 1 ? p.least[at] : r;
-      key = (uint32_t)first << 13 | (uint32_t)r;
+  int grouped = 0;
+  auto key_of = [&](int32_t r) {
+    const int32_t at = slot_of[r];
+    const int32_t first = at >= 0 && members[least[at]] > 1 ? least[at] : r;
+    grouped |= first != r;
+    return (uint32_t)first << 13 | (uint32_t)r;
+  };
+  if (kFits) {
+    // (a key's place is the number of smaller ones: fewer barriers than a sort's steps)
+    for (int32_t r = tid; r < n; r += kThreads) unsorted[r] = key_of(r);
+    const bool sort = __syncthreads_or(grouped);
+    for (int32_t r = tid; r < n; r += kThreads) {
+      const uint32_t key = unsorted[r];
+      int32_t at = r;
+      if (sort) {
+        at = 0;
+        for (int32_t i = 0; i < n; ++i) at += unsorted[i] < key;
+      }
+      keys[at] = key;
     }
-    keys[r] = key;
-  }
-  for (int32_t k = 2; k <= n2; k <<= 1)
-    for (int32_t j = k >> 1; j > 0; j >>= 1) {
-      __syncthreads();
-      for (int32_t i = tid; i < n2; i += kThreads) {
-        const int32_t o = i ^ j;
-        if (o > i) {
-          const uint32_t x = keys[i], y = keys[o];
-          if ((x > y) == ((i & k) == 0)) {
-            keys[i] = y;
-            keys[o] = x;
+  } else {
+    int32_t n2 = 64;
+    while (n2 < n) n2 <<= 1;
+    for (int32_t r = tid; r < n2; r += kThreads) keys[r] = r < n ? key_of(r) : 0xFFFFFFFFu;
+    if (__syncthreads_or(grouped))
+      for (int32_t k = 2; k <= n2; k <<= 1)
+        for (int32_t j = k >> 1; j > 0; j >>= 1) {
+          __syncthreads();
+          for (int32_t i = tid; i < n2; i += kThreads) {
+            const int32_t o = i ^ j;
+            if (o > i) {
+              const uint32_t x = keys[i], y = keys[o];
+              if ((x > y) == ((i & k) == 0)) {
+                keys[i] = y;
+                keys[o] = x;
+              }
+            }
           }
         }
-      }
-    }
+  }
   __syncthreads();
+  auto rows_of = [&](int32_t i) {
+    const int32_t r = keys[i] & 8191u;
+    return w.row_off[r + 1] - w.row_off[r];
+  };
   scan_all(
-      n, sums, [&](int32_t i) { return (int64_t)(w.row_off[(keys[i] & 8191u) + 1] - w.row_off[keys[i] & 8191u]); },
-      [&](int32_t i, int64_t at) { p.base[i] = (int32_t)at; });
+      n, sums, [&](int32_t i) { return (int64_t)rows_of(i); }, [&](int32_t i, int64_t at) { base[i] = (int32_t)at; });
   __syncthreads();
 
   // Segments, and the rows in their order.
   auto write_row = [&](int32_t i, const BlockReq& q, bool ok, int32_t j) {
-    const int32_t at = p.base[i] + j;
+    const int32_t at = base[i] + j;
     const int64_t lim = (int64_t)q.ctx - (q.hi - q.lo) + j + 1;
     p.row[at] = q.lo + j;
     p.lim[at] = ok && lim > 0 ? (int32_t)lim : 0;
-    p.place[at] = i;
+  };
+  auto tiles_of = [&](AttendSeg* s) {
+    s->wide = (int64_t)s->tokens * ratio > kNarrowRows;
+    s->tiles = s->wide ? (int32_t)(((int64_t)s->tokens * ratio + kWideRows - 1) / kWideRows) : 1;
   };
   for (int32_t i = tid; i < n; i += kThreads) {
     const int32_t r = keys[i] & 8191u, first = keys[i] >> 13;
     const BlockReq q = block_req(w, r);
     const bool ok = p.flags[r] == 0;
     const int32_t rows = q.hi - q.lo;
-    const bool shared = p.slot_of[r] >= 0 && p.members[first] > 1;
-    p.order[i] = r;
-    AttendSeg s{};
+    const bool shared = slot_of[r] >= 0 && members[first] > 1;
+    AttendSeg s{}, none{};
     s.pre_off = q.pre_off;
     s.tail_off = q.tail_off;
     s.pre_len = q.pre_len;
     s.shared = shared;
     const int32_t pre = shared ? q.pre_len * w.bt : 0;
     AttendSeg own = s;
-    own.p0 = p.base[i];
+    own.p0 = base[i];
     own.tokens = rows;
     own.t0 = pre;
     own.t1 = ok && rows > 0 ? q.ctx : 0;
-    const bool some = own.t1 > own.t0;
-    own.wide = (int64_t)rows * ratio > kNarrowRows;
-    own.tiles = !some ? 0 : own.wide ? (int32_t)(((int64_t)rows * ratio + kWideRows - 1) / kWideRows) : 1;
+    tiles_of(&own);
+    if (own.t1 <= own.t0) own.tiles = 0;
     p.segs[2 * i + 1] = own;
-    p.segs[2 * i] = AttendSeg{};
     int32_t lead = -1;
     if (shared) {
       // the place of the group's first member: of the keys, the least with this first
@@ -198,15 +274,15 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
       }
       lead = a;
       if (lead == i) {
-        const int32_t last = i + p.members[first] - 1, lr = keys[last] & 8191u;
-        s.p0 = p.base[i];
-        s.tokens = p.base[last] + (w.row_off[lr + 1] - w.row_off[lr]) - s.p0;
+        const int32_t last = i + members[first] - 1;
+        s.p0 = base[i];
+        s.tokens = base[last] + rows_of(last) - s.p0;
         s.t1 = pre;
-        s.wide = (int64_t)s.tokens * ratio > kNarrowRows;
-        s.tiles = s.wide ? (int32_t)(((int64_t)s.tokens * ratio + kWideRows - 1) / kWideRows) : 1;
-        p.segs[2 * i] = s;
+        tiles_of(&s);
+        none = s;
       }
     }
+    p.segs[2 * i] = none;
     p.lead[i] = lead;
     if (rows <= 8) {
       for (int32_t j = 0; j < rows; ++j) write_row(i, q, ok, j);
@@ -221,20 +297,16 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
     const bool ok = p.flags[r] == 0;
     for (int32_t j = lane; j < q.hi - q.lo; j += 64) write_row(i, q, ok, j);
   }
-  __syncthreads();
 
-  // Tiles.
+  // Tiles, those of both kinds counted in one sum.
+  const int64_t counts = scan_all(
+      2 * n, sums,
+      [&](int32_t k) { return p.segs[k].wide ? (int64_t)p.segs[k].tiles : (int64_t)p.segs[k].tiles << 32; },
+      [&](int32_t k, int64_t at) { p.segs[k].tile0 = p.segs[k].wide ? (int32_t)at : (int32_t)(at >> 32); });
+  const int32_t n_tiles[2] = {(int32_t)counts, (int32_t)(counts >> 32)};
   if (tid == 0) n_todo = 0;
-  int32_t n_tiles[2];
-  for (int kind = 0; kind < 2; ++kind)
-    n_tiles[kind] = (int32_t)scan_all(
-        2 * n, sums,
-        [&](int32_t k) { return (int64_t)(p.segs[k].wide == (kind == 0) ? p.segs[k].tiles : 0); },
-        [&](int32_t k, int64_t at) {
-          if (p.segs[k].wide == (kind == 0)) p.segs[k].tile0 = (int32_t)at;
-        });
   __syncthreads();
-  auto write_tile = [&](const AttendSeg& s, int32_t k, int32_t prefix) {
+  auto write_tile = [&](const AttendSeg& s, int32_t k, int32_t seg) {
     AttendTile t{};
     t.pre_off = s.pre_off;
     t.tail_off = s.tail_off;
@@ -246,52 +318,69 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
     // (a request's later rows see more: none of the tile's sees more than its last)
     t.t1 = min(s.t1, p.lim[s.p0 + (t.row0 + t.rows - 1) / ratio]);
     t.shared = s.shared;
-    t.prefix = prefix;
+    t.prefix = !(seg & 1);
+    t.pre_tile = -1;
+    if (s.shared && !t.prefix) {
+      const AttendSeg& l = p.segs[2 * p.lead[seg / 2]];
+      t.pre_tile = l.wide ? l.tile0 | kWideBit : l.tile0;
+      t.pre_p0 = l.p0;
+    }
     p.tiles[s.wide ? 0 : 1][s.tile0 + k] = t;
   };
   for (int32_t k = tid; k < 2 * n; k += kThreads) {
     const AttendSeg s = p.segs[k];
     if (s.tiles <= 4)
-      for (int32_t j = 0; j < s.tiles; ++j) write_tile(s, j, !(k & 1));
+      for (int32_t j = 0; j < s.tiles; ++j) write_tile(s, j, k);
     else
       p.todo[atomicAdd(&n_todo, 1)] = k;
   }
   __syncthreads();
   for (int32_t k = wave; k < n_todo; k += kWaves) {
-    const AttendSeg s = p.segs[p.todo[k]];
-    for (int32_t j = lane; j < s.tiles; j += 64) write_tile(s, j, !(p.todo[k] & 1));
+    const int32_t seg = p.todo[k];
+    const AttendSeg s = p.segs[seg];
+    for (int32_t j = lane; j < s.tiles; j += 64) write_tile(s, j, seg);
   }
   __syncthreads();
 
-  // Units end to end, who takes them, and the rows of partial results.
+  // Units end to end, and who takes them.
   AttendHead h{};
-  int64_t units[2];
-  auto units_of = [&](const AttendTile& t) { return (int64_t)((max(0, t.t1 - t.t0) + kUnit - 1) / kUnit); };
+  int64_t units[2], wide_cost = 0;
+  int64_t* begin[2];
+  int64_t* run_at[2];
   for (int kind = 0; kind < 2; ++kind) {
-    h.n_tiles[kind] = n_tiles[kind];
+    begin[kind] = n_tiles[kind] <= kNear ? near_begin[kind] : p.begin[kind];
+    int64_t mine = 0;
     units[kind] = scan_all(
-        n_tiles[kind], sums, [&](int32_t k) { return units_of(p.tiles[kind][k]); },
-        [&](int32_t k, int64_t at) { p.begin[kind][k] = at; });
+        n_tiles[kind], sums,
+        [&](int32_t k) {
+          const AttendTile& t = p.tiles[kind][k];
+          const int64_t u = units_of(t);
+          mine += u * (kUnitCost + t.rows);
+          return u;
+        },
+        [&](int32_t k, int64_t at) { begin[kind][k] = at; });
+    if (kind == 0 && n_tiles[0] > 4 * kThreads) mine /= 2;  // (each value was asked for twice)
+    if (kind == 0 && n_tiles[0] > 0 && n_tiles[1] > 0) block_scan(mine, &wide_cost, sums);
+    h.n_tiles[kind] = n_tiles[kind];
   }
   {
-    int64_t mine = 0, wide;
-    for (int32_t k = tid; k < n_tiles[0]; k += kThreads) mine += units_of(p.tiles[0][k]) * (kUnitCost + p.tiles[0][k].rows);
-    block_scan(mine, &wide, sums);
-    const int64_t all = wide + kUnitCost * units[1];
-    int64_t n_wide = all > 0 ? (wide * p.groups + all / 2) / all : 0;
-    if (units[0] > 0) n_wide = max(n_wide, (int64_t)1);
-    if (units[1] > 0) n_wide = min(n_wide, (int64_t)p.groups - 1);
-    h.wide_groups = h.runs[0] = (int32_t)n_wide;
+    int64_t n_wide = units[0] > 0 ? p.groups : 0;
+    if (units[0] > 0 && units[1] > 0) {
+      const int64_t all = wide_cost + kUnitCost * units[1];
+      n_wide = min(max((wide_cost * p.groups + all / 2) / all, (int64_t)1), (int64_t)p.groups - 1);
+    }
+    h.wide_groups = (int32_t)n_wide;
+    h.runs[0] = (int32_t)min(n_wide, units[0]);
     h.runs[1] = (int32_t)min((p.groups - n_wide) * kWavesPerGroup, units[1]);
   }
+  for (int kind = 0; kind < 2; ++kind) run_at[kind] = h.runs[kind] <= kNear ? near_run[kind] : p.run_at[kind];
   __syncthreads();
   // Rounds of whole tiles, as many as leave no workgroup (a thread each) above
   // the average; then `share` units more for each, the most evenly.
-  int64_t share = 0;
-  if (h.wide_groups > 0) {
+  if (h.wide_groups > 0 && n_tiles[0] >= h.wide_groups) {
     const int32_t n_wide = h.wide_groups;
     const bool mine = tid < n_wide;
-    int64_t whole = 0, total;
+    int64_t whole = 0, total, share = 0;
     for (h.rounds = n_tiles[0] / n_wide;; --h.rounds) {
       whole = 0;
       for (int32_t i = 0; mine && i < h.rounds; ++i) whole += units_of(p.tiles[0][tid + i * n_wide]);
@@ -312,54 +401,53 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
     // (left / n_below each, the first left % n_below one more)
     const int64_t rank = block_scan(below ? 1 : 0, &total, sums);
     if (below) share = left / n_below + (rank < left % n_below) - whole;
+    const int32_t done = h.rounds * n_wide;
+    const int64_t skip = done < n_tiles[0] ? begin[0][done] : units[0];
+    const int64_t at = block_scan(share, &total, sums), number = block_scan(share > 0, &total, sums);
+    h.runs[0] = n_wide;
+    if (mine) {
+      run_at[0][tid] = skip + at;
+      p.runs[0][tid].units = (int32_t)share;
+      p.runs[0][tid].number = (int32_t)number;
+    }
+  } else {
+    for (int32_t r = tid; r < h.runs[0]; r += kThreads) {
+      run_at[0][r] = units[0] * r / h.runs[0];
+      p.runs[0][r].units = (int32_t)(units[0] * (r + 1) / h.runs[0] - units[0] * r / h.runs[0]);
+      p.runs[0][r].number = r;
+    }
   }
-  int64_t slots = 0;
+  for (int32_t r = tid; r < h.runs[1]; r += kThreads) {
+    run_at[1][r] = units[1] * r / h.runs[1];
+    p.runs[1][r].units = (int32_t)(units[1] * (r + 1) / h.runs[1] - units[1] * r / h.runs[1]);
+    p.runs[1][r].number = r;
+  }
+  __syncthreads();
   for (int kind = 0; kind < 2; ++kind) {
     AttendTile* tiles = p.tiles[kind];
     const int32_t whole = kind == 0 ? h.rounds * h.wide_groups : 0, runs = h.runs[kind];
-    const int64_t skip = whole < n_tiles[kind] ? p.begin[kind][whole] : units[kind];
-    if (kind == 0) {
-      int64_t total;
-      const int64_t at = block_scan(share, &total, sums), number = block_scan(share > 0, &total, sums);
-      if (tid < runs) {
-        p.run_at[0][tid] = skip + at;
-        p.runs[0][tid].units = (int32_t)share;
-        p.runs[0][tid].number = (int32_t)number;
-      }
-    } else {
-      for (int32_t r = tid; r < runs; r += kThreads) {
-        p.run_at[1][r] = units[1] * r / runs;
-        p.runs[1][r].units = (int32_t)(units[1] * (r + 1) / runs - units[1] * r / runs);
-        p.runs[1][r].number = r;
-      }
-    }
-    __syncthreads();
     for (int32_t r = tid; r < runs; r += kThreads) {
-      const int64_t at = p.run_at[kind][r];
-      int32_t a = 0, b = n_tiles[kind];  // the last tile that begins at or before `at`
-      while (b - a > 1) {
-        const int32_t m = (a + b) >> 1;
-        if (p.begin[kind][m] <= at) a = m;
-        else b = m;
-      }
-      p.runs[kind][r].tile = a;
-      p.runs[kind][r].from = (int32_t)(at - p.begin[kind][a]);
+      const int64_t at = run_at[kind][r];
+      const int32_t k = last_at_most(begin[kind], n_tiles[kind], at);
+      p.runs[kind][r].tile = k;
+      p.runs[kind][r].from = (int32_t)(at - begin[kind][k]);
     }
-    auto run_of = [&](int64_t u) {  // the last run that begins at or before unit u
-      int32_t a = 0, b = runs;
-      while (b - a > 1) {
-        const int32_t m = (a + b) >> 1;
-        if (p.run_at[kind][m] <= u) a = m;
-        else b = m;
-      }
-      return p.runs[kind][a].number;
-    };
     for (int32_t k = tid; k < n_tiles[kind]; k += kThreads) {
-      const int64_t u = units_of(tiles[k]), b = p.begin[kind][k];
-      tiles[k].first = u > 0 && k >= whole ? run_of(b) : 0;
-      tiles[k].pieces = u == 0 ? 0 : k < whole ? 1 : run_of(b + u - 1) - tiles[k].first + 1;
+      const int64_t u = units_of(tiles[k]), b = begin[kind][k];
+      int32_t first = 0, pieces = u > 0 ? 1 : 0;
+      if (u > 0 && k >= whole) {
+        // (a run that begins at the same unit as the next one is empty and not found)
+        first = p.runs[kind][last_at_most(run_at[kind], runs, b)].number;
+        pieces = p.runs[kind][last_at_most(run_at[kind], runs, b + u - 1)].number - first + 1;
+      }
+      tiles[k].first = first;
+      tiles[k].pieces = pieces;
     }
-    __syncthreads();
+  }
+  __syncthreads();
+  int64_t slots = 0;
+  for (int kind = 0; kind < 2; ++kind) {
+    AttendTile* tiles = p.tiles[kind];
     const int64_t before = slots;
     // (kept where there are two pieces or more, or one of a shared segment.  One
     // comparison of a sum: of the same test with && and ||, the compiler dropped the
@@ -372,7 +460,6 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
         [&](int32_t k, int64_t at) {
           tiles[k].slot = tiles[k].pieces + tiles[k].shared > 1 ? (int32_t)(before + at) : -1;
         });
-    __syncthreads();
   }
 
   // What is to be joined: the rows of own tiles that are kept, with their prefix
@@ -380,36 +467,45 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
   // alone; of everything else that has no pieces, places of empty rows.
   if (tid == 0) n_todo = 0;
   __syncthreads();
-  auto push = [&](int32_t place, int32_t sub, int32_t own) {
-    AttendJoin x{place, sub, {own, -1}};
-    const int32_t lead = sub < 0 ? -1 : p.lead[p.place[place]];
-    if (lead >= 0) {
-      const AttendSeg& s = p.segs[2 * lead];
-      x.tile[1] = s.wide ? (s.tile0 + ((place - s.p0) * ratio + sub) / kWideRows) | kWideBit : s.tile0;
-    }
-    p.joins[atomicAdd(&n_todo, 1)] = x;
+  // (place's row `sub` of the prefix whose first tile and place these are)
+  auto prefix_tile = [&](int32_t pre_tile, int32_t pre_p0, int32_t place, int32_t sub) {
+    if (pre_tile < 0 || !(pre_tile & kWideBit)) return pre_tile;
+    return pre_tile + ((place - pre_p0) * ratio + sub) / kWideRows;
+  };
+  auto push = [&](int32_t place, int32_t sub, int32_t own, int32_t prefix) {
+    p.joins[atomicAdd(&n_todo, 1)] = AttendJoin{place, sub, {own, prefix}};
   };
   for (int kind = 0; kind < 2; ++kind) {
-    // a wave per wide tile, a quarter of one per narrow tile
-    const int per = kind == 0 ? 64 : 16;
+    // a wave per wide tile, 4 lanes per narrow tile
+    const int per = kind == 0 ? 64 : 4;
     for (int32_t k = tid / per; k < n_tiles[kind]; k += kThreads / per) {
-      const AttendTile t = p.tiles[kind][k];
+      const AttendTile& t = p.tiles[kind][k];
       if (t.prefix || (t.pieces > 0 && t.slot < 0)) continue;
-      for (int32_t r = tid % per; r < t.rows; r += per) {
-        const int32_t x = t.row0 + r, at = x / ratio, sub = x - at * ratio;
-        if (t.pieces > 0) push(t.p0 + at, sub, kind == 0 ? k | kWideBit : k);
-        else if (sub == 0 || r == 0) push(t.p0 + at, -1, -1);
+      const int32_t rows = t.rows, row0 = t.row0, p0 = t.p0, pieces = t.pieces, pre_tile = t.pre_tile, pre_p0 = t.pre_p0;
+      for (int32_t r = tid % per; r < rows; r += per) {
+        const int32_t x = row0 + r, at = x / ratio, sub = x - at * ratio;
+        if (pieces > 0)
+          push(p0 + at, sub, kind == 0 ? k | kWideBit : k, prefix_tile(pre_tile, pre_p0, p0 + at, sub));
+        else if (sub == 0 || r == 0)
+          push(p0 + at, -1, -1, -1);
       }
     }
   }
   for (int32_t i = wave; i < n; i += kWaves) {
     const AttendSeg& s = p.segs[2 * i + 1];
     if (s.tiles > 0) continue;
+    int32_t pre_tile = -1, pre_p0 = 0;
+    if (s.shared) {
+      const AttendSeg& l = p.segs[2 * p.lead[i]];
+      pre_tile = l.wide ? l.tile0 | kWideBit : l.tile0;
+      pre_p0 = l.p0;
+    }
     for (int32_t j = lane; j < s.tokens; j += 64)
       if (s.shared)
-        for (int32_t sub = 0; sub < ratio; ++sub) push(s.p0 + j, sub, -1);
+        for (int32_t sub = 0; sub < ratio; ++sub)
+          push(s.p0 + j, sub, -1, prefix_tile(pre_tile, pre_p0, s.p0 + j, sub));
       else
-        push(s.p0 + j, -1, -1);
+        push(s.p0 + j, -1, -1, -1);
   }
   __syncthreads();
   h.n_joins = n_todo;
@@ -423,6 +519,9 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
 hipError_t ps_launch_attend_plan(const ps::AttendPlanDev& p, const ps::BlockWin& w, int32_t ratio, uint32_t* d_flags,
                                  hipStream_t s) {
   hipLaunchKernelGGL(ps::plan_check_kernel, dim3(w.n_req), dim3(256), 0, s, p, w, d_flags);
-  hipLaunchKernelGGL(ps::plan_cut_kernel, dim3(1), dim3(ps::kThreads), 0, s, p, w, ratio, d_flags);
+  if (p.table_mask < 2 * ps::kSmall)
+    hipLaunchKernelGGL(ps::plan_cut_kernel<true>, dim3(1), dim3(ps::kThreads), 0, s, p, w, ratio, d_flags);
+  else
+    hipLaunchKernelGGL(ps::plan_cut_kernel<false>, dim3(1), dim3(ps::kThreads), 0, s, p, w, ratio, d_flags);
   return hipGetLastError();
 }

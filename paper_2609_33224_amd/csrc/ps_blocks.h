@@ -121,6 +121,8 @@ struct AttendSeg {
   int32_t wide, shared;
 };
 
+constexpr int32_t kWideBit = 1 << 30;  // a tile's number: it is a wide one's
+
 struct AttendTile {
   int64_t pre_off, tail_off;
   int32_t pre_len, p0;
@@ -131,6 +133,8 @@ struct AttendTile {
   int32_t slot;    // first row of the partial results, `rows` per piece; -1: written out directly
   int32_t shared;  // its rows have another segment
   int32_t prefix;  // it is a shared prefix's
+  // of an own tile of a shared segment: the prefix's first tile (| kWideBit) and place
+  int32_t pre_tile, pre_p0;
   int32_t pad;
 };
 
@@ -141,7 +145,6 @@ struct alignas(16) AttendJoin {
   int32_t sub;      // query head of the group; -1: all of them, empty
   int32_t tile[2];  // own, prefix: place in the list of its kind | kWideBit; -1: none
 };
-constexpr int32_t kWideBit = 1 << 30;
 
 struct AttendHead {
   int32_t n_joins;
@@ -165,14 +168,12 @@ struct AttendPlanDev {
   int32_t* least;     // per slot: the least request
   int32_t* slot_of;   // per request: its slot, -1 for none
   int32_t* members;   // per request: of the group it leads
-  int32_t* order;     // requests, groups together, by their least member
-  int32_t* base;      // per place of `order`: first of its rows in the row order
-  int32_t* lead;      // per place of `order`: the place of its group's first member, -1 unshared
+  int32_t* base;      // per request in the order of the groups: first of its rows in the row order
+  int32_t* lead;      // likewise: the place of its group's first member, -1 unshared
   int32_t* row;       // row order: row of the window
   int32_t* lim;       // positions it sees
-  int32_t* place;     // its request's place in `order`
   int32_t* todo;      // requests, later segments, with much to write
-  AttendSeg* segs;    // 2 per place: prefix (first members only), own
+  AttendSeg* segs;    // 2 per request, in that order: prefix (first members only), own
   AttendTile* tiles[2];
   int64_t* begin[2];  // first unit of each tile
   AttendRun* runs[2];

@@ -127,12 +127,10 @@ hipError_t each_buffer(ps_attend_plan* p, F f) {
   one(d.least, (size_t)d.table_mask + 1);
   one(d.slot_of, n);
   one(d.members, n);
-  one(d.order, n);
   one(d.base, n);
   one(d.lead, n);
   one(d.row, rows);
   one(d.lim, rows);
-  one(d.place, rows);
   one(d.todo, 2 * n);
   one(d.segs, 2 * n);
   for (int k = 0; k < 2; ++k) {
