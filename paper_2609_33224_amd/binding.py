@@ -384,6 +384,7 @@ class KvCache:
             raise ValueError("exponents belong to float8_e4m3fn caches")
         self.tensors = (k, v, k_exp, v_exp)
         self.device = k.device
+        self.shape = (heads, dim)
         self.dtype = k.dtype
         self.raw = PsKvCache(k.data_ptr(), v.data_ptr(), *[x.data_ptr() if x is not None else None for x in exps],
                              pages, max(k.stride(0), heads * block * dim), stride, heads, dim, block,
@@ -422,32 +423,40 @@ class KvWindow:
                               self.n_req, self.n_rows)
 
 
-def _same_device(*things):
-    if len({t.device for t in things if t is not None}) != 1:
-        raise ValueError("tensors on different devices")
+def _same_device(device, *things):
+    for t in things:
+        if t is not None and t.device != device:
+            raise ValueError("tensors on different devices")
 
 
 def _block_stream(stream, device) -> int:
     return (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream
 
 
-def _rows(t: torch.Tensor, name: str, n_rows: int, heads: int, dim: int) -> PsRows:
-    if t.dim() != 3 or t.shape[0] < n_rows or tuple(t.shape[1:]) != (heads, dim):
+def _rows(t: torch.Tensor, name: str, device, n_rows: int, heads: int, dim: int) -> PsRows:
+    # (a call of one step takes a few microseconds on the GPU: each attribute is asked for once)
+    shape, strides, dtype = t.shape, t.stride(), _ROW_TYPES.get(t.dtype)
+    if len(shape) != 3 or shape[0] < n_rows or shape[1] != heads or shape[2] != dim:
         raise ValueError(f"{name} must be (at least {n_rows} rows, {heads} heads, {dim})")
-    if t.dtype not in _ROW_TYPES or not t.is_cuda or (t.numel() and t.stride(2) != 1):
+    if t.device != device:
+        raise ValueError("tensors on different devices")
+    if dtype is None or (strides[2] != 1 and t.numel()):
         raise ValueError(f"{name} must be a bfloat16 or float16 device tensor, contiguous in its last axis")
     # (an axis of one entry has no stride that matters)
-    row = t.stride(0) if t.shape[0] > 1 else max(8, heads * dim)
-    head = t.stride(1) if heads > 1 else dim
-    return PsRows(t.data_ptr(), row, head, _ROW_TYPES[t.dtype])
+    return PsRows(t.data_ptr(), strides[0] if shape[0] > 1 else max(8, heads * dim),
+                  strides[1] if heads > 1 else dim, dtype)
 
 
 def _kv_rows(call, ctx, cache: KvCache, window: KvWindow, k, v, stream) -> None:
-    _same_device(cache, window, k, v)
-    shape = (window.n_rows, cache.raw.n_kv_heads, cache.raw.head_dim)
-    rk, rv = _rows(k, "k", *shape), _rows(v, "v", *shape)
-    _check(ctx, call(ctx, ctypes.byref(cache.raw), ctypes.byref(window.raw), ctypes.byref(rk), ctypes.byref(rv),
-                     _block_stream(stream, cache.device)))
+    device, raw, n = cache.device, cache.raw, window.n_rows
+    if window.device != device:
+        raise ValueError("tensors on different devices")
+    heads, dim = cache.shape
+    rk, rv = _rows(k, "k", device, n, heads, dim), _rows(v, "v", device, n, heads, dim)
+    code = call(ctx, ctypes.byref(raw), ctypes.byref(window.raw), ctypes.byref(rk), ctypes.byref(rv),
+                _block_stream(stream, device))
+    if code:
+        _check(ctx, code)
 
 
 def ps_kv_write_dev(ctx, cache: KvCache, window: KvWindow, k: torch.Tensor, v: torch.Tensor, stream=None) -> None:
@@ -498,8 +507,7 @@ class AttendPlan:
         """Plan `window`; d_flags (uint32 or int32, one per request): PS_R_INVALID for malformed requests."""
         if d_flags is not None and (d_flags.element_size() != 4 or d_flags.numel() < window.n_req):
             raise ValueError("d_flags must hold 32 bits per request")
-        if d_flags is not None:
-            _same_device(window, d_flags)
+        _same_device(window.device, d_flags)
         _check(self.scorer.ctx, load_library().ps_attend_plan_dev(
             self._handle(), ctypes.byref(window.raw), _dev_ptr(d_flags), _block_stream(stream, window.device)))
         self.window = window
@@ -514,11 +522,14 @@ class AttendPlan:
         if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape[1:]) != (heads,)
                                 or lse.dim() != 2 or lse.shape[0] < n_rows):
             raise ValueError("lse must be float32 (rows, heads)")
-        _same_device(cache, q, out, lse, self.window)
-        rq, ro = _rows(q, "q", n_rows, heads, dim), _rows(out, "out", n_rows, heads, dim)
-        _check(self.scorer.ctx, load_library().ps_attend_window_dev(
+        device = cache.device
+        _same_device(device, lse, self.window)
+        rq, ro = _rows(q, "q", device, n_rows, heads, dim), _rows(out, "out", device, n_rows, heads, dim)
+        code = load_library().ps_attend_window_dev(
             self._handle(), ctypes.byref(cache.raw), ctypes.byref(rq), ctypes.byref(ro), _dev_ptr(lse),
-            float(dim ** -0.5 if scale is None else scale), _block_stream(stream, cache.device)))
+            dim ** -0.5 if scale is None else scale, _block_stream(stream, device))
+        if code:
+            _check(self.scorer.ctx, code)
 
 
 # ------------------------------------------------------------------ tensors

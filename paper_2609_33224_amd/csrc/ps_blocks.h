@@ -72,11 +72,10 @@ __host__ __device__ inline int32_t block_row_req(const BlockWin& w, int32_t row)
   return w.row_off[a] <= row && row < w.row_off[a + 1] ? a : -1;
 }
 
-// Where row `row` of the window lies: its page and slot; false where it has
-// none.  *has_req: whether a request claims the row.
-__host__ __device__ inline bool block_locate(const BlockWin& w, int32_t row, bool* has_req, int64_t* page,
+// Where row `row` of the window, of request r, lies: its page and slot; false where it
+// has none.  *has_req: whether a request claims the row.
+__host__ __device__ inline bool block_locate(const BlockWin& w, int32_t row, int32_t r, bool* has_req, int64_t* page,
                                              int32_t* slot) {
-  const int32_t r = block_row_req(w, row);
   *has_req = r >= 0;
   if (r < 0) return false;
   const BlockReq q = block_req(w, r);
@@ -109,6 +108,7 @@ constexpr int kWavesPerGroup = 4;
 // Cost of a unit for a workgroup, in rows: of a narrow tile's (1.5 to 1.75 us of e4m3
 // with every workgroup at work), and what a wide one's has beside its rows (3.7 us for 128).
 constexpr int kUnitCost = 128;
+constexpr int kWideTileCost = 256, kTileCost = 160;  // of a tile beside its units: lookups, q, results
 constexpr int kShareMinTokens = 64;  // of a prefix
 constexpr int kShareMaxRows = 64;    // of a member (or one row of all its heads)
 

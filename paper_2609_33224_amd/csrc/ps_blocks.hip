@@ -292,7 +292,8 @@ ps_status ps_attend_window_dev(ps_attend_plan* p, const ps_kv_cache* cache, cons
 // request, 1 for a row without a place, 2 and *page, *slot otherwise.
 int32_t ps_test_block_locate(const ps_kv_window* w, int32_t block_tokens, int32_t row, int64_t* page, int32_t* slot) {
   bool has = false;
-  const bool at = block_locate(dev_win(*w, block_tokens), row, &has, page, slot);
+  const BlockWin win = dev_win(*w, block_tokens);
+  const bool at = block_locate(win, row, block_row_req(win, row), &has, page, slot);
   return at ? 2 : has ? 1 : 0;
 }
 

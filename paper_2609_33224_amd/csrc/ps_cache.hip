@@ -73,12 +73,39 @@ __device__ inline Unit unit_of(const BlockCache& c, const Place& mine, int32_t r
   return u;
 }
 
+// The request of row row0 + lane, for the first `per` lanes (block_row_req, by the wave:
+// it looks at 64 offsets at a time, so that a window of 4,096 requests takes two
+// rounds where a search by halves takes twelve).
+__device__ inline int32_t rows_req(const BlockWin& w, int32_t row0, int32_t per) {
+  const int lane = threadIdx.x & 63;
+  int32_t a = 0, b = w.n_req;  // the last request that begins at or before row0 is in [a, b)
+  while (b - a > 64) {
+    const int32_t step = (b - a + 63) / 64, at = a + lane * step;
+    const uint64_t hit = __ballot(at < b && w.row_off[at] <= row0);
+    // (offsets that ascend make it a prefix; any other answer is checked below)
+    const int32_t last = hit ? 63 - __builtin_clzll(hit) : 0;
+    a += last * step;
+    b = min(b, a + step);
+  }
+  // of 64 requests from there on: how many begin at or before each row
+  const int32_t off = a + lane < w.n_req ? w.row_off[a + lane] : INT32_MAX;
+  int32_t r = -1;
+  for (int32_t i = 0; i < per; ++i) {
+    const uint64_t hit = __ballot(a + lane < w.n_req && off <= row0 + i);
+    if (lane == i) r = hit >> 63 ? -2 : hit ? a + 63 - __builtin_clzll(hit) : -1;  // -2: maybe a later one
+  }
+  if (lane >= per || row0 + lane >= w.n_rows) return -1;
+  if (r == -2) return block_row_req(w, row0 + lane);
+  return r >= 0 && w.row_off[r] <= row0 + lane && row0 + lane < w.row_off[r + 1] ? r : -1;
+}
+
 __device__ inline Place place_of(const BlockWin& w, int32_t row0, int32_t per) {
   const int lane = threadIdx.x & 63;
   Place p{0, 0, 0};
+  const int32_t r = rows_req(w, row0, per);
   if (lane < per && row0 + lane < w.n_rows) {
     bool has;
-    const bool in = block_locate(w, row0 + lane, &has, &p.page, &p.slot);
+    const bool in = block_locate(w, row0 + lane, r, &has, &p.page, &p.slot);
     p.state = in ? 2 : has ? 1 : 0;
     if (!in) {
       p.page = 0;
