@@ -718,19 +718,14 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_kernel(AttendAr
   p.c = fmaxf(fabsf(c), 1.17549435e-38f);  // (not 0: it multiplies infinities)
   p.neg = c < 0 ? 0x80008000u : 0u;
   // (scalars throughout: what is loaded after the first store would be a lane's otherwise)
-  const AttendHead& h = *a.plan.head;
-  const int32_t wide_groups = uniform(h.wide_groups);
-  const int kind = group >= wide_groups;
-  // (the waves' runs go round the workgroups)
-  const int32_t r = kind == 0 ? group : group - wide_groups + wave * (a.plan.groups - wide_groups);
-  if (r >= uniform(h.runs[kind])) return;  // (of a wide tile's workgroup, all waves or none)
-  const AttendRun run = a.plan.runs[kind][r];
-  const int32_t rounds = kind == 0 ? uniform(h.rounds) : 0, number = uniform(run.number);
-  int32_t next = uniform(run.tile), at = uniform(run.from), left = uniform(run.units);
+  const AttendRun run = a.plan.runs[group * kWavesPerGroup + wave];
+  const int32_t kind = uniform(run.kind), rounds = uniform(run.rounds), number = uniform(run.number);
+  int32_t next = uniform(run.next), at = uniform(run.from), left = uniform(run.units);
   for (int32_t round = 0;;) {
+    const bool first = round == 0 && left == run.units;
     int32_t k, from, most, piece;
     if (round < rounds) {
-      k = r + round++ * wide_groups;
+      k = group + round++ * uniform(run.stride);
       from = piece = 0;
       most = INT32_MAX;
     } else {
@@ -741,8 +736,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_kernel(AttendAr
       piece = number;
       at = 0;
     }
-    const AttendTile* tiles = a.plan.tiles[kind];
-    const AttendTile t = tiles[k];
+    AttendTile t = run.tile;
+    if (!uniform((int32_t)first)) t = a.plan.tiles[kind][k];
     const int32_t t0 = uniform(t.t0), t1 = uniform(t.t1), slot = uniform(t.slot);
     const int32_t n = min(max(0, (t1 - t0 + kUnit - 1) / kUnit) - from, most);
     if (n <= 0) continue;  // (a tile of no positions)
@@ -766,12 +761,13 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_kernel(AttendAr
 // head, and writes the rows that nothing was computed for.  Where there are no more rows than
 // workgroups (a few long contexts, cut into many pieces), a row is a workgroup's: its
 // waves take every fourth run of 64 / LG * kAtOnce pieces; otherwise a wave's.  LG lanes
-// hold a row of results, so 64 / LG pieces are read at once, kAtOnce times.
+// hold a row of results, so 64 / LG pieces are read at once, kAtOnce times; their maxima
+// and sums come with them, one pass with a running maximum.
 template <bool kF16, int LG>
 __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
   constexpr int kAtOnce = 4, kStep = 64 / LG, kRun = kAtOnce * kStep;
   __shared__ f32x4 rows[3][LG];
-  __shared__ float sums[4];
+  __shared__ float2 mls[4];
   const int lane = threadIdx.x & 63, sub = lane / LG, d = 4 * (lane % LG);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int32_t D = a.cache.dim;
@@ -781,7 +777,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
   for (int64_t id = first; id < n; id += (int64_t)gridDim.x * (together ? 1 : 4)) {
     const AttendJoin x = a.plan.joins[id / a.cache.heads];
     const int32_t head = (int32_t)(id % a.cache.heads);
-    const int64_t row = a.plan.row[x.place];
+    const int64_t row = x.row, slots = (int64_t)head * a.plan.slot_rows;
     const bool writes = !together || wave == 0;
     if (x.sub < 0) {
       for (int32_t h = head * a.ratio; writes && h < (head + 1) * a.ratio; ++h) {
@@ -791,28 +787,13 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
       }
       continue;
     }
-    const bool empty = a.plan.lim[x.place] <= 0;
-    int64_t from[2] = {0, 0};
-    int32_t count[2] = {0, 0}, step[2] = {0, 0};
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      if (x.tile[k] < 0) continue;
-      const AttendTile& t = a.plan.tiles[x.tile[k] & kWideBit ? 0 : 1][x.tile[k] & (kWideBit - 1)];
-      count[k] = t.pieces;
-      step[k] = t.rows;
-      from[k] = (int64_t)head * a.plan.slot_rows + t.slot + ((x.place - t.p0) * a.ratio + x.sub - t.row0);
-    }
-    const int32_t total = count[0] + count[1];
+    const int32_t total = x.count[0] + x.count[1];
     auto slot = [&](int32_t j) {
-      const bool own = j < count[0];
-      return (own ? from[0] : from[1]) + (int64_t)(own ? j : j - count[0]) * (own ? step[0] : step[1]);
+      const bool own = j < x.count[0];
+      return slots + (own ? x.from[0] : x.from[1]) + (int64_t)(own ? j : j - x.count[0]) * (own ? x.step[0] : x.step[1]);
     };
-    float top = -INFINITY;
-    for (int32_t j = lane; j < total; j += 64) top = fmaxf(top, a.plan.part_ml[slot(j)].x);
-    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-    const float mc = top == -INFINITY ? 0.0f : top;
     f32x4 acc = {0, 0, 0, 0};
-    float l = 0;
+    float m = -INFINITY, l = 0;  // the lane's, of its every kStep-th piece
     for (int32_t j = together ? wave * kRun : 0; j < total; j += together ? 4 * kRun : kRun) {
       f32x4 o[kAtOnce];
       float2 ml[kAtOnce];
@@ -827,6 +808,13 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
           if (d < D) o[u] = *(const f32x4*)(a.plan.part + s * D + d);
         }
       }
+      float nm = m;
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) nm = fmaxf(nm, ml[u].x);
+      const float mc = nm == -INFINITY ? 0.0f : nm, g = __builtin_amdgcn_exp2f(m - mc);
+      m = nm;
+      l *= g;
+      acc *= g;
 #pragma unroll
       for (int u = 0; u < kAtOnce; ++u) {
         const float f = __builtin_amdgcn_exp2f(ml[u].x - mc);
@@ -835,6 +823,17 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
         for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(o[u][e], f, acc[e]);
       }
     }
+    float top = m;
+#pragma unroll
+    for (int o = LG; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+    if (together) {
+      if (lane == 0) mls[wave].x = top;
+      __syncthreads();
+      top = fmaxf(fmaxf(mls[0].x, mls[1].x), fmaxf(mls[2].x, mls[3].x));
+    }
+    const float f = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.0f : top));
+    l *= f;
+    acc *= f;
 #pragma unroll
     for (int o = LG; o < 64; o <<= 1) {
       l += __shfl_xor(l, o, 64);
@@ -843,9 +842,9 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
     }
     if (together) {
       if (wave > 0 && sub == 0) rows[wave - 1][lane % LG] = acc;
-      if (lane == 0) sums[wave] = l;
+      if (lane == 0) mls[wave].y = l;
       __syncthreads();
-      l = sums[0] + sums[1] + sums[2] + sums[3];
+      l = mls[0].y + mls[1].y + mls[2].y + mls[3].y;
 #pragma unroll
       for (int w = 0; w < 3; ++w) acc += rows[w][lane % LG];
       __syncthreads();
@@ -854,19 +853,18 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
     const float inv = 1.0f / l;
     if (writes && sub == 0 && d < D) {
       u32x2 w = {0, 0};
-      if (!empty) w = u32x2{pack<kF16>(acc[0] * inv, acc[1] * inv), pack<kF16>(acc[2] * inv, acc[3] * inv)};
+      if (!x.empty) w = u32x2{pack<kF16>(acc[0] * inv, acc[1] * inv), pack<kF16>(acc[2] * inv, acc[3] * inv)};
       *(u32x2*)(a.out.data + 2 * (row * a.out.row + (int64_t)h * a.out.head + d)) = w;
     }
     if (writes && a.lse && lane == 0)
-      a.lse[row * a.heads + h] = empty ? -INFINITY : __builtin_fmaf(top, kLn2, __logf(l));
+      a.lse[row * a.heads + h] = x.empty ? -INFINITY : __builtin_fmaf(top, kLn2, __logf(l));
   }
 }
 
 template <bool kF16, bool kQ8, int DP>
 void launch(const AttendArgs& a, int32_t num_cus, hipStream_t s) {
   const dim3 grid((unsigned)(a.plan.groups * a.cache.heads));
-  const int64_t rows = (int64_t)a.win.n_rows * a.heads;
-  const dim3 join((unsigned)std::min<int64_t>((rows + 3) / 4, 8 * num_cus));
+  const dim3 join((unsigned)std::min<int64_t>((int64_t)a.win.n_rows * a.heads, 8 * num_cus));
   hipLaunchKernelGGL((attend_kernel<kF16, kQ8, DP>), grid, dim3(256), 0, s, a);
   hipLaunchKernelGGL((join_kernel<kF16, DP / 4>), join, dim3(256), 0, s, a);
 }

@@ -125,6 +125,7 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
   __shared__ int32_t near_table[kFits ? 2 * kSmall : 1], near_least[kFits ? 2 * kSmall : 1];
   __shared__ int32_t near_slot[kFits ? kSmall : 1], near_members[kFits ? kSmall : 1], near_base[kFits ? kSmall : 1];
   __shared__ int64_t near_begin[2][kNear], near_run[2][kNear];
+  __shared__ int32_t wide_number[kThreads], wide_units[kThreads];
   __shared__ int64_t sums[kWaves];
   __shared__ int32_t n_todo;
   int32_t* const table = kFits ? near_table : p.table;
@@ -151,6 +152,7 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
     if (d_flags)
       for (int32_t r = tid; r < n; r += kThreads) d_flags[r] = PS_R_INVALID;
     if (tid == 0) *p.head = AttendHead{};
+    for (int32_t x = tid; x < p.groups * kWavesPerGroup; x += kThreads) p.runs[x].rounds = p.runs[x].units = 0;
     return;
   }
 
@@ -343,7 +345,7 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
   __syncthreads();
 
   // Units end to end, and who takes them.
-  AttendHead h{};
+  int32_t wide_groups, rounds = 0, runs[2];
   int64_t units[2], wide_cost = 0;
   int64_t* begin[2];
   int64_t* run_at[2];
@@ -361,7 +363,6 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
         [&](int32_t k, int64_t at) { begin[kind][k] = at; });
     if (kind == 0 && n_tiles[0] > 4 * kThreads) mine /= 2;  // (each value was asked for twice)
     if (kind == 0 && n_tiles[0] > 0 && n_tiles[1] > 0) block_scan(mine, &wide_cost, sums);
-    h.n_tiles[kind] = n_tiles[kind];
   }
   {
     int64_t n_wide = units[0] > 0 ? p.groups : 0;
@@ -372,22 +373,22 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
       n_wide = max(wide_cost * p.groups / all, (int64_t)1);
       n_wide = min(n_wide, (int64_t)p.groups - 1);
     }
-    h.wide_groups = (int32_t)n_wide;
-    h.runs[0] = (int32_t)min(n_wide, units[0]);
-    h.runs[1] = (int32_t)min((p.groups - n_wide) * kWavesPerGroup, units[1]);
+    wide_groups = (int32_t)n_wide;
+    runs[0] = (int32_t)min(n_wide, units[0]);
+    runs[1] = (int32_t)min((p.groups - n_wide) * kWavesPerGroup, units[1]);
   }
-  for (int kind = 0; kind < 2; ++kind) run_at[kind] = h.runs[kind] <= kNear ? near_run[kind] : p.run_at[kind];
+  for (int kind = 0; kind < 2; ++kind) run_at[kind] = runs[kind] <= kNear ? near_run[kind] : p.run_at[kind];
   __syncthreads();
   // Rounds of whole tiles, as many as leave no workgroup (a thread each) above
   // the average; then `share` units more for each, the most evenly.
-  if (h.wide_groups > 0 && n_tiles[0] >= h.wide_groups) {
-    const int32_t n_wide = h.wide_groups;
+  if (wide_groups > 0 && n_tiles[0] >= wide_groups) {
+    const int32_t n_wide = wide_groups;
     const bool mine = tid < n_wide;
     int64_t whole = 0, total, share = 0;
-    for (h.rounds = n_tiles[0] / n_wide;; --h.rounds) {
+    for (rounds = n_tiles[0] / n_wide;; --rounds) {
       whole = 0;
-      for (int32_t i = 0; mine && i < h.rounds; ++i) whole += units_of(p.tiles[0][tid + i * n_wide]);
-      if (!__syncthreads_or(mine && h.rounds > 0 && whole * n_wide > units[0])) break;
+      for (int32_t i = 0; mine && i < rounds; ++i) whole += units_of(p.tiles[0][tid + i * n_wide]);
+      if (!__syncthreads_or(mine && rounds > 0 && whole * n_wide > units[0])) break;
     }
     // a level that those below it are filled up to
     int64_t left = units[0], n_below = n_wide;
@@ -404,46 +405,40 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
     // (left / n_below each, the first left % n_below one more)
     const int64_t rank = block_scan(below ? 1 : 0, &total, sums);
     if (below) share = left / n_below + (rank < left % n_below) - whole;
-    const int32_t done = h.rounds * n_wide;
+    const int32_t done = rounds * n_wide;
     const int64_t skip = done < n_tiles[0] ? begin[0][done] : units[0];
     const int64_t at = block_scan(share, &total, sums), number = block_scan(share > 0, &total, sums);
-    h.runs[0] = n_wide;
+    runs[0] = n_wide;
     if (mine) {
       run_at[0][tid] = skip + at;
-      p.runs[0][tid].units = (int32_t)share;
-      p.runs[0][tid].number = (int32_t)number;
+      wide_units[tid] = (int32_t)share;
+      wide_number[tid] = (int32_t)number;
     }
   } else {
-    for (int32_t r = tid; r < h.runs[0]; r += kThreads) {
-      run_at[0][r] = units[0] * r / h.runs[0];
-      p.runs[0][r].units = (int32_t)(units[0] * (r + 1) / h.runs[0] - units[0] * r / h.runs[0]);
-      p.runs[0][r].number = r;
+    for (int32_t r = tid; r < runs[0]; r += kThreads) {
+      run_at[0][r] = units[0] * r / runs[0];
+      wide_units[r] = (int32_t)(units[0] * (r + 1) / runs[0] - units[0] * r / runs[0]);
+      wide_number[r] = r;
     }
   }
   // (counting a tile as a unit more made a batch of short contexts no faster, and one of
   // long ones slower: 241 -> 246 us)
-  for (int32_t r = tid; r < h.runs[1]; r += kThreads) {
-    run_at[1][r] = units[1] * r / h.runs[1];
-    p.runs[1][r].units = (int32_t)(units[1] * (r + 1) / h.runs[1] - units[1] * r / h.runs[1]);
-    p.runs[1][r].number = r;
-  }
+  for (int32_t r = tid; r < runs[1]; r += kThreads) run_at[1][r] = units[1] * r / runs[1];
   __syncthreads();
   for (int kind = 0; kind < 2; ++kind) {
     AttendTile* tiles = p.tiles[kind];
-    const int32_t whole = kind == 0 ? h.rounds * h.wide_groups : 0, runs = h.runs[kind];
-    for (int32_t r = tid; r < runs; r += kThreads) {
-      const int64_t at = run_at[kind][r];
-      const int32_t k = last_at_most(begin[kind], n_tiles[kind], at);
-      p.runs[kind][r].tile = k;
-      p.runs[kind][r].from = (int32_t)(at - begin[kind][k]);
-    }
+    const int32_t whole = kind == 0 ? rounds * wide_groups : 0;
+    // (a run that begins at the same unit as the next one is empty and not found)
+    auto number_at = [&](int64_t u) {
+      const int32_t r = last_at_most(run_at[kind], runs[kind], u);
+      return kind == 0 ? wide_number[r] : r;
+    };
     for (int32_t k = tid; k < n_tiles[kind]; k += kThreads) {
       const int64_t u = units_of(tiles[k]), b = begin[kind][k];
       int32_t first = 0, pieces = u > 0 ? 1 : 0;
       if (u > 0 && k >= whole) {
-        // (a run that begins at the same unit as the next one is empty and not found)
-        first = p.runs[kind][last_at_most(run_at[kind], runs, b)].number;
-        pieces = p.runs[kind][last_at_most(run_at[kind], runs, b + u - 1)].number - first + 1;
+        first = number_at(b);
+        pieces = number_at(b + u - 1) - first + 1;
       }
       tiles[k].first = first;
       tiles[k].pieces = pieces;
@@ -467,32 +462,63 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
         });
   }
 
+  // What each wave takes.
+  __syncthreads();
+  for (int32_t x = tid; x < p.groups * kWavesPerGroup; x += kThreads) {
+    const int32_t g = x / kWavesPerGroup, kind = g >= wide_groups;
+    // (the waves' runs go round the workgroups)
+    const int32_t r = kind == 0 ? g : g - wide_groups + x % kWavesPerGroup * (p.groups - wide_groups);
+    AttendRun run{};
+    run.kind = kind;
+    if (r < runs[kind]) {
+      run.rounds = kind == 0 ? rounds : 0;
+      run.stride = wide_groups;
+      run.number = kind == 0 ? wide_number[r] : r;
+      const int64_t at = run_at[kind][r];
+      run.units = kind == 0 ? wide_units[r] : (int32_t)((r + 1 < runs[1] ? run_at[1][r + 1] : units[1]) - at);
+      if (run.units > 0) {
+        run.next = last_at_most(begin[kind], n_tiles[kind], at);
+        run.from = (int32_t)(at - begin[kind][run.next]);
+      }
+      if (run.rounds > 0 || run.units > 0) run.tile = p.tiles[kind][run.rounds > 0 ? r : run.next];
+    }
+    p.runs[x] = run;
+  }
+
   // What is to be joined: the rows of own tiles that are kept, with their prefix
   // tiles; of shared segments that end with the prefix, the rows with the prefix
   // alone; of everything else that has no pieces, places of empty rows.
   if (tid == 0) n_todo = 0;
   __syncthreads();
-  // (place's row `sub` of the prefix whose first tile and place these are)
-  auto prefix_tile = [&](int32_t pre_tile, int32_t pre_p0, int32_t place, int32_t sub) {
-    if (pre_tile < 0 || !(pre_tile & kWideBit)) return pre_tile;
-    return pre_tile + ((place - pre_p0) * ratio + sub) / kWideRows;
-  };
-  auto push = [&](int32_t place, int32_t sub, int32_t own, int32_t prefix) {
-    p.joins[atomicAdd(&n_todo, 1)] = AttendJoin{place, sub, {own, prefix}};
+  // (pre_tile, pre_p0: the prefix's first tile and place)
+  auto push = [&](int32_t place, int32_t sub, const AttendTile* own, int32_t pre_tile, int32_t pre_p0) {
+    AttendJoin x{};
+    x.row = p.row[place];
+    x.sub = sub;
+    x.empty = p.lim[place] <= 0;
+    auto part = [&](int i, const AttendTile& t) {
+      x.from[i] = t.slot + (place - t.p0) * ratio + sub - t.row0;
+      x.count[i] = t.pieces;
+      x.step[i] = t.rows;
+    };
+    if (own) part(0, *own);
+    if (pre_tile >= 0) {
+      const int32_t k = pre_tile & (kWideBit - 1);
+      if (pre_tile & kWideBit) part(1, p.tiles[0][k + ((place - pre_p0) * ratio + sub) / kWideRows]);
+      else part(1, p.tiles[1][k]);
+    }
+    p.joins[atomicAdd(&n_todo, 1)] = x;
   };
   for (int kind = 0; kind < 2; ++kind) {
     // a wave per wide tile, 4 lanes per narrow tile
     const int per = kind == 0 ? 64 : 4;
     for (int32_t k = tid / per; k < n_tiles[kind]; k += kThreads / per) {
-      const AttendTile& t = p.tiles[kind][k];
+      const AttendTile t = p.tiles[kind][k];
       if (t.prefix || (t.pieces > 0 && t.slot < 0)) continue;
-      const int32_t rows = t.rows, row0 = t.row0, p0 = t.p0, pieces = t.pieces, pre_tile = t.pre_tile, pre_p0 = t.pre_p0;
-      for (int32_t r = tid % per; r < rows; r += per) {
-        const int32_t x = row0 + r, at = x / ratio, sub = x - at * ratio;
-        if (pieces > 0)
-          push(p0 + at, sub, kind == 0 ? k | kWideBit : k, prefix_tile(pre_tile, pre_p0, p0 + at, sub));
-        else if (sub == 0 || r == 0)
-          push(p0 + at, -1, -1, -1);
+      for (int32_t r = tid % per; r < t.rows; r += per) {
+        const int32_t x = t.row0 + r, at = x / ratio, sub = x - at * ratio;
+        if (t.pieces > 0) push(t.p0 + at, sub, &t, t.pre_tile, t.pre_p0);
+        else if (sub == 0 || r == 0) push(t.p0 + at, -1, nullptr, -1, 0);
       }
     }
   }
@@ -507,14 +533,12 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
     }
     for (int32_t j = lane; j < s.tokens; j += 64)
       if (s.shared)
-        for (int32_t sub = 0; sub < ratio; ++sub)
-          push(s.p0 + j, sub, -1, prefix_tile(pre_tile, pre_p0, s.p0 + j, sub));
+        for (int32_t sub = 0; sub < ratio; ++sub) push(s.p0 + j, sub, nullptr, pre_tile, pre_p0);
       else
-        push(s.p0 + j, -1, -1, -1);
+        push(s.p0 + j, -1, nullptr, -1, 0);
   }
   __syncthreads();
-  h.n_joins = n_todo;
-  if (tid == 0) *p.head = h;
+  if (tid == 0) *p.head = AttendHead{n_todo};
 }
 
 }  // namespace

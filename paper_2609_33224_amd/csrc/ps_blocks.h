@@ -138,27 +138,30 @@ struct AttendTile {
   int32_t pad;
 };
 
-// What the second kernel joins: one row of a tile, or all rows of a place that
-// nothing was computed for.
+// What the second kernel joins for one row of the window and one of the group's query
+// heads (sub; -1: all of them, nothing was computed): the rows from[i], from[i] + step[i],
+// .. of partial results, count[i] of them, of its own segment and of its prefix.
 struct alignas(16) AttendJoin {
-  int32_t place;    // in the row order
-  int32_t sub;      // query head of the group; -1: all of them, empty
-  int32_t tile[2];  // own, prefix: place in the list of its kind | kWideBit; -1: none
+  int32_t row, sub;
+  int32_t from[2], count[2], step[2];
+  int32_t empty;  // the row sees no position
+  int32_t pad[3];
 };
 
 struct AttendHead {
   int32_t n_joins;
-  int32_t n_tiles[2];   // wide, narrow
-  int32_t wide_groups;  // workgroups per head that take wide tiles; the others take narrow ones
-  int32_t rounds;       // whole wide tiles that each of them takes first: its number + i wide_groups
-  int32_t runs[2];      // wide_groups; waves that take narrow ones
 };
 
-// Units that a workgroup (after its rounds) or a wave takes.
+// What a wave of a workgroup takes: (wide tiles, all four waves the same) `rounds` whole
+// tiles, its own number + i stride, then `units` from unit `from` of tile `next` on.
+// The first tile's record is here too, so that a wave has one lookup less to wait for.
 struct alignas(16) AttendRun {
-  int32_t tile, from;  // first tile, the first unit of it
-  int32_t units;       // in all; 0: none
-  int32_t number;      // of the runs of its kind that have units
+  AttendTile tile;
+  int32_t number;  // of the runs of its kind that have units
+  int32_t kind;    // 0: wide, 1: narrow
+  int32_t rounds, stride;
+  int32_t next, from, units;
+  int32_t pad[3];
 };
 
 struct AttendPlanDev {
@@ -176,8 +179,8 @@ struct AttendPlanDev {
   AttendSeg* segs;    // 2 per request, in that order: prefix (first members only), own
   AttendTile* tiles[2];
   int64_t* begin[2];  // first unit of each tile
-  AttendRun* runs[2];
-  int64_t* run_at[2];  // first unit of each run
+  AttendRun* runs;     // of wave w of workgroup g: 4 g + w
+  int64_t* run_at[2];  // first unit of each run, wide and narrow
   AttendJoin* joins;
   float* part;        // partial results: [head][slot rows][dim], weights as numerators
   float2* part_ml;    // their maxima (times scale * log2 e) and sums

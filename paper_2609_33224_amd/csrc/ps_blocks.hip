@@ -136,10 +136,10 @@ hipError_t each_buffer(ps_attend_plan* p, F f) {
   for (int k = 0; k < 2; ++k) {
     one(d.tiles[k], d.tile_cap[k]);
     one(d.begin[k], d.tile_cap[k]);
-    one(d.runs[k], (size_t)d.groups * (k == 0 ? 1 : kWavesPerGroup));
     one(d.run_at[k], (size_t)d.groups * (k == 0 ? 1 : kWavesPerGroup));
   }
   // (a row with partial results each, or a place of empty rows: twice where two tiles have some)
+  one(d.runs, (size_t)d.groups * kWavesPerGroup);
   one(d.joins, (size_t)d.slot_rows + rows + d.tile_cap[0]);
   one(d.part, part * p->dim);
   one(d.part_ml, part);
