@@ -222,10 +222,9 @@ __device__ inline void put4(const AttendArgs& a, const Piece& p, int32_t r, int3
   *(u32x2*)(a.out.data + 2 * ((int64_t)a.plan.row[w.place] * a.out.row + (int64_t)w.head * a.out.head + d)) = x;
 }
 
-// A row's maximum (of scores) and sum, likewise; returns what its results are
+// A row's maximum (mc: of scores times c) and sum, likewise; returns what its results are
 // multiplied by where they are final.
-__device__ inline float put_ml(const AttendArgs& a, const Piece& p, int32_t r, float m, float l, bool write) {
-  const float mc = m == -INFINITY ? -INFINITY : m * p.c;
+__device__ inline float put_ml(const AttendArgs& a, const Piece& p, int32_t r, float mc, float l, bool write) {
   if (p.slot >= 0) {
     if (write) a.plan.part_ml[(int64_t)p.head * a.plan.slot_rows + p.slot + r] = float2{mc, l};
     return 1.0f;
@@ -454,7 +453,7 @@ __device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char*
     l[b] += __shfl_xor(l[b], 32, 64);
     const int32_t r = b * 16 + (at & 15);
     if (r < p.rows) {
-      const float inv = put_ml(a, p, r, m[b], l[b], d0 == 0);
+      const float inv = put_ml(a, p, r, m[b] == -INFINITY ? -INFINITY : m[b] * p.c, l[b], d0 == 0);
 #pragma unroll
       for (int k = 0; k < kDB; ++k) put4<kF16>(a, p, r, 16 * k + d0, acc[b][k], inv);
     }
@@ -491,7 +490,7 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
   for (int k = 0; k < kDB; ++k)
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[k][i] = 0;
-  float m = -INFINITY, l = 0;
+  float m = -INFINITY, l = 0;  // (the maximum of scores times c)
 
   // staging: thread x takes row x / kPer of the positions, chunks x % kPer + kPer i
   const int srow = wave * (64 / kPer) + lane / kPer, sc = lane % kPer;
@@ -596,14 +595,19 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
 #pragma unroll
       for (int i = 1; i < kMine / 2; ++i) top = fmaxf(top, s[i >> 4][i & 15]);
       top = fmaxf(top, __shfl_xor(top, 32, 64));
-      const float nm = fmaxf(m, top), mc = nm == -INFINITY ? 0.0f : nm * p.c;
-      if (__any(nm > m)) {  // (a factor of 1 otherwise)
-        const float f = __builtin_amdgcn_exp2f(__builtin_fmaf(m, p.c, -mc));
+      // The maximum that weights are taken from follows the row's own only where that is 2^8
+      // above it: weights of up to 256 fit both types and are rounded to as many bits, and of
+      // 32 rows in random order one has a new maximum in most steps, none so large a one.
+      const float tc = top * p.c;
+      const bool up = tc > m + 8.0f;
+      if (__any(up)) {
+        const float f = up ? __builtin_amdgcn_exp2f(m - tc) : 1.0f;
+        m = up ? tc : m;
         l *= f;
 #pragma unroll
         for (int k = 0; k < kDB; ++k) acc[k] *= f;
       }
-      m = nm;
+      const float mc = m == -INFINITY ? 0.0f : m;
       if (masked && odd_at[buf] == t)
 #pragma unroll 1
         for (int32_t o = t + off0; o < min(t + off0 + kMine, p.tb); ++o)
@@ -668,9 +672,9 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
     __syncthreads();
     if (!(wave & 1)) {
       const float2 x = ml[r];
-      const float top = fmaxf(m, x.x), mc = top == -INFINITY ? 0.0f : top * p.c;
-      const float f = __builtin_amdgcn_exp2f(__builtin_fmaf(m, p.c, -mc));
-      const float fx = __builtin_amdgcn_exp2f(__builtin_fmaf(x.x, p.c, -mc));
+      const float top = fmaxf(m, x.x), mc = top == -INFINITY ? 0.0f : top;
+      const float f = __builtin_amdgcn_exp2f(m - mc);
+      const float fx = __builtin_amdgcn_exp2f(x.x - mc);
       l = l * f + x.y * fx;
       m = top;
 #pragma unroll
