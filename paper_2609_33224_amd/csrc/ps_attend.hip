@@ -17,6 +17,8 @@
 //  - A wide tile (128 rows: a prefix that many requests share, a prompt) is
 //    bound by the matrix cores: 64 positions are staged in shared memory for the four
 //    waves, which have 32 rows each.
+//  - In windows of long prompts such tiles are tall, 256 rows for eight waves, which
+//    take turns with the matrix cores.
 // e4m3 values are brought to the 16-bit type with their power of two as they
 // are staged (exact but for fp16's range), so one kernel serves both.
 
@@ -465,42 +467,27 @@ __device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char*
 // Positions of a wide step: 64, or 32 where a row's registers leave no room.
 constexpr int wide_positions(int DP) { return DP <= 128 ? 64 : 32; }
 
-// kSplit = 1: each wave has 32 of the 128 rows and all positions of a step; 2: 32 of 64
-// rows and half of the positions, the halves' results joined at the end, so that
-// tiles of 64 rows keep all four SIMDs at work.
-template <bool kF16, bool kQ8, int DP, int kSplit>
-__device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* smem, int32_t* odd_at) {
-  constexpr int kSteps = DP / 16;
-  constexpr int kTok = wide_positions(DP);
-  constexpr int kPer = 256 / kTok;                               // threads that stage a row
-  constexpr int kLoads = (kQ8 ? DP / 16 : DP / 8) / kPer;  // 16-byte loads per thread
-  constexpr int kDB = DP / 32;
-  constexpr int kK = key_stride(DP), kV = value_stride(DP);
-  constexpr int kKeys = kTok * kK, kTile = kTok * (kK + kV);  // bytes of a step's keys; of all
-  constexpr int kMine = kTok / kSplit;  // positions of a step that are the wave's
-  const int lane = fresh(threadIdx.x & 63), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int col = lane & 31, hb = lane >> 5;
-  const int D = a.cache.dim;
-  const int rows0 = wave / kSplit * 32, off0 = wave % kSplit * kMine;
-  const int32_t r = rows0 + col;
-  const bool idle = rows0 >= p.rows;
-
-  f32x16 acc[kDB];
-#pragma unroll
-  for (int k = 0; k < kDB; ++k)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) acc[k][i] = 0;
-  float m = -INFINITY, l = 0;  // (the maximum of scores times c)
-
-  // staging: thread x takes row x / kPer of the positions, chunks x % kPer + kPer i
-  const int srow = wave * (64 / kPer) + lane / kPer, sc = lane % kPer;
-  const int32_t last = p.tb - 1;
+// What a thread of a wide or tall tile's workgroup stages: part of one row of a step's
+// positions, asked for (pages, then loads) before it is put into shared memory.
+template <bool kF16, bool kQ8, int DP, int kTok, int kThreads>
+struct Stage {
+  static constexpr int kPer = kThreads / kTok;                     // threads that stage a row
+  static constexpr int kLoads = (kQ8 ? DP / 16 : DP / 8) / kPer;  // 16-byte loads per thread
+  static constexpr int kChunk = kQ8 ? 32 : 16;                     // bytes in shared memory of such a load
+  const int row, sc;  // thread x: row x / kPer, chunks x % kPer + kPer i
+  const int32_t last;
   uint32_t page;
   u32x4 kr[kLoads], vr[kLoads];
   uint32_t kx = 0, vx = 0;
-  auto pages = [&](int32_t t) { page = page_of(a, p.chain, min(t + srow, last)); };
-  auto loads = [&](int32_t t) {
-    const Spot s = spot_of(a, p.head, page, min(t + srow, last));
+
+  __device__ Stage(const Piece& p, int wave, int lane)
+      : row(wave * (64 / kPer) + lane / kPer), sc(lane % kPer), last(p.tb - 1) {}
+  __device__ void pages(const AttendArgs& a, const Piece& p, int32_t t) {
+    page = page_of(a, p.chain, min(t + row, last));
+  }
+  __device__ void loads(const AttendArgs& a, const Piece& p, int32_t t) {
+    const Spot s = spot_of(a, p.head, page, min(t + row, last));
+    const int D = a.cache.dim;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int d = kQ8 ? min(16 * (kPer * i + sc), D - 16) : min(8 * (kPer * i + sc), D - 8);  // (as in the narrow kernel)
@@ -512,23 +499,22 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
       kx = a.cache.kx[s.x];
       vx = a.cache.vx[s.x];
     }
-  };
-  // (of one request's rows the first sees least; those of a shared prefix see all of it)
-  const int32_t least_of_all = a.plan.lim[row_at(a, p, 0).place];
-  auto stage = [&](int buf, int32_t t) {
-    const bool masked = t + kTok > p.tb || t + kTok > least_of_all;
+  }
+  // Into the step's keys and values; whether values had infinities or NaN, which are
+  // taken out of a masked step's (as in the narrow kernel).
+  __device__ uint32_t put(unsigned char* keys, unsigned char* values, bool masked) {
     uint32_t odd = 0;
-    unsigned char* ks = smem + buf * kTile + srow * kK + sc * (kQ8 ? 32 : 16);
-    unsigned char* vs = smem + buf * kTile + kKeys + srow * kV + sc * (kQ8 ? 32 : 16);
+    unsigned char* ks = keys + row * key_stride(DP) + sc * kChunk;
+    unsigned char* vs = values + row * value_stride(DP) + sc * kChunk;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int off = kPer * (kQ8 ? 32 : 16) * i;
+      const int off = kPer * kChunk * i;
       if (kQ8) {
         const float sk = scale_of(kx), sv = scale_of(vx);
         *(u32x4*)(ks + off) = widen8<kF16>(kr[i][0], kr[i][1], sk);
         *(u32x4*)(ks + off + 16) = widen8<kF16>(kr[i][2], kr[i][3], sk);
         u32x4 x = widen8<kF16>(vr[i][0], vr[i][1], sv), y = widen8<kF16>(vr[i][2], vr[i][3], sv);
-        if (masked) {  // (as in the narrow kernel)
+        if (masked) {
           odd |= clean8<kF16>(x);
           odd |= clean8<kF16>(y);
         }
@@ -540,16 +526,133 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
         *(u32x4*)(vs + off) = vr[i];
       }
     }
-    if (odd) odd_at[buf] = t;  // (a value left by another piece only costs a look)
+    return odd;
+  }
+};
+
+// A wave's scores of 32 kB positions from t, lane: position 32 b + 8 (i / 4) + 4 hb + i % 4:
+// those that the row does not see are taken out.
+template <int kB>
+__device__ inline void mask_scores(f32x16 (&s)[kB], int32_t t, int hb, int32_t end) {
+#pragma unroll
+  for (int b = 0; b < kB; ++b)
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (t + 32 * b + 8 * (i >> 2) + 4 * hb + (i & 3) >= end) s[b][i] = -INFINITY;
+}
+
+// The running maximum (m, of scores times c) after these scores; the sum and the results follow it.
+// It follows the row's own only where that is 2^8 above it: weights of up to 256 fit both
+// types and are rounded to as many bits, and of 32 rows in random order one has a new
+// maximum in most steps, none so large a one.
+template <int kB, int kDB>
+__device__ inline void follow_top(const f32x16 (&s)[kB], float c, float& m, float& l, f32x16 (&acc)[kDB]) {
+  float top = s[0][0];
+#pragma unroll
+  for (int i = 1; i < 16 * kB; ++i) top = fmaxf(top, s[i >> 4][i & 15]);
+  top = fmaxf(top, __shfl_xor(top, 32, 64));
+  const float tc = top * c;
+  const bool up = tc > m + 8.0f;
+  if (__any(up)) {
+    const float f = up ? __builtin_amdgcn_exp2f(m - tc) : 1.0f;
+    m = up ? tc : m;
+    l *= f;
+#pragma unroll
+    for (int k = 0; k < kDB; ++k) acc[k] *= f;
+  }
+}
+
+// The infinities and NaN that were taken out of positions [t, end)'s values, to the rows that see them.
+template <bool kF16, bool kQ8, int kDB>
+__device__ inline void add_odd(const AttendArgs& a, const Piece& p, int32_t t, int32_t end, int hb, int32_t lim,
+                               f32x16 (&acc)[kDB]) {
+#pragma unroll 1
+  for (int32_t o = t; o < end; ++o)
+#pragma unroll
+    for (int k = 0; k < 4 * kDB; ++k) {
+      const f32x4 x = odd_values<kF16, kQ8>(a, p, o, min(8 * k + fresh(4 * hb), a.cache.dim - 4));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[k >> 2][4 * (k & 3) + i] = added(acc[k >> 2][4 * (k & 3) + i], o < lim ? x[i] : 0.0f);
+    }
+}
+
+// Weights of a wave's scores 16 x .. 16 x + 15, packed; their sum is added to *sum.
+template <bool kF16, int kB>
+__device__ inline u32x4 weights(const f32x16 (&s)[kB], int x, float c, float mc, float* sum) {
+  u32x4 w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int at = (x & 1) * 8 + 2 * i;
+    const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x >> 1][at], c, -mc));
+    const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x >> 1][at + 1], c, -mc));
+    *sum += e0 + e1;
+    w[i] = pack<kF16>(e0, e1);
+  }
+  return w;
+}
+
+// The results of a wave's 32 rows from rows0.
+template <bool kF16, int kDB>
+__device__ inline void put_rows(const AttendArgs& a, const Piece& p, int rows0, int lane, float m, float l,
+                                const f32x16 (&acc)[kDB]) {
+  const int at = fresh(lane), d0 = 4 * (at >> 5);
+  const int32_t r = rows0 + (at & 31);
+  if (r >= p.rows) return;
+  const float inv = put_ml(a, p, r, m, l, d0 == 0);
+#pragma unroll
+  for (int k = 0; k < kDB; ++k)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      put4<kF16>(a, p, r, 32 * k + 8 * i + d0,
+                 f32x4{acc[k][4 * i], acc[k][4 * i + 1], acc[k][4 * i + 2], acc[k][4 * i + 3]}, inv);
+}
+
+// Elements 32 k + (lane's column) of 16 positions' values, turned: positions 8 jj + 4 hb ..
+__device__ inline u32x4 turned_values(const unsigned char* at, int stride) {
+  const u32x2 y0 = read_turned(at), y1 = read_turned(at + 8 * stride);
+  return u32x4{y0[0], y0[1], y1[0], y1[1]};
+}
+
+// kSplit = 1: each wave has 32 of the 128 rows and all positions of a step; 2: 32 of 64
+// rows and half of the positions, the halves' results joined at the end, so that
+// tiles of 64 rows keep all four SIMDs at work.
+template <bool kF16, bool kQ8, int DP, int kSplit>
+__device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* smem, int32_t* odd_at) {
+  constexpr int kSteps = DP / 16;
+  constexpr int kTok = wide_positions(DP);
+  constexpr int kDB = DP / 32;
+  constexpr int kK = key_stride(DP), kV = value_stride(DP);
+  constexpr int kKeys = kTok * kK, kTile = kTok * (kK + kV);  // bytes of a step's keys; of all
+  constexpr int kMine = kTok / kSplit;  // positions of a step that are the wave's
+  const int lane = fresh(threadIdx.x & 63), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 31, hb = lane >> 5;
+  const int rows0 = wave / kSplit * 32, off0 = wave % kSplit * kMine;
+  const int32_t r = rows0 + col;
+  const bool idle = rows0 >= p.rows;
+
+  f32x16 acc[kDB];
+#pragma unroll
+  for (int k = 0; k < kDB; ++k)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[k][i] = 0;
+  float m = -INFINITY, l = 0;  // (the maximum of scores times c)
+
+  Stage<kF16, kQ8, DP, kTok, 256> st(p, wave, lane);
+  // (of one request's rows the first sees least; those of a shared prefix see all of it)
+  const int32_t least_of_all = a.plan.lim[row_at(a, p, 0).place];
+  auto stage = [&](int buf, int32_t t) {
+    unsigned char* keys = smem + buf * kTile;
+    if (st.put(keys, keys + kKeys, t + kTok > p.tb || t + kTok > least_of_all))
+      odd_at[buf] = t;  // (a value left by another piece only costs a look)
   };
 
   // (the order: as in the narrow kernel)
-  pages(p.ta);
+  st.pages(a, p, p.ta);
   const RowAt qrow = row_at(a, p, min(r, p.rows - 1));
   int32_t lim = a.plan.lim[qrow.place];
   const int64_t qat = a.plan.row[qrow.place] * a.q.row + (int64_t)qrow.head * a.q.head;
-  loads(p.ta);
-  pages(p.ta + kTok);
+  st.loads(a, p, p.ta);
+  st.pages(a, p, p.ta + kTok);
   // (heads above 128: no registers for q, it stays in shared memory)
   u32x4 q[DP <= 128 ? kSteps : 1];
   unsigned char* qs = smem + 2 * kTile + (wave * 32 + col) * kK + hb * 16;
@@ -566,8 +669,8 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
   __syncthreads();
   int buf = 0;
   for (int32_t t = p.ta; t < p.tb; t += kTok, buf ^= 1) {
-    loads(t + kTok);  // (behind the last step too: as in the narrow kernel)
-    pages(t + 2 * kTok);
+    st.loads(a, p, t + kTok);  // (behind the last step too: as in the narrow kernel)
+    st.pages(a, p, t + 2 * kTok);
     if (!idle) {
       const unsigned char* ks = smem + buf * kTile + (off0 + col) * kK + hb * 16;
       const unsigned char* vs =
@@ -579,50 +682,17 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[b][i] = 0;
 #pragma unroll
-        for (int st = 0; st < kSteps; ++st)
-          s[b] = mfma32<kF16>(*(const u32x4*)(ks + 32 * b * kK + 32 * st),
-                              DP <= 128 ? q[DP <= 128 ? st : 0] : *(const u32x4*)(qs + 32 * st), s[b]);
+        for (int i = 0; i < kSteps; ++i)
+          s[b] = mfma32<kF16>(*(const u32x4*)(ks + 32 * b * kK + 32 * i),
+                              DP <= 128 ? q[DP <= 128 ? i : 0] : *(const u32x4*)(qs + 32 * i), s[b]);
       }
       const bool masked = t + kTok > p.tb || t + kTok > least;
-      if (masked) {
-#pragma unroll
-        for (int b = 0; b < kMine / 32; ++b)
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (t + off0 + 32 * b + 8 * (i >> 2) + 4 * hb + (i & 3) >= min(lim, p.tb)) s[b][i] = -INFINITY;
-      }
-      float top = s[0][0];
-#pragma unroll
-      for (int i = 1; i < kMine / 2; ++i) top = fmaxf(top, s[i >> 4][i & 15]);
-      top = fmaxf(top, __shfl_xor(top, 32, 64));
-      // The maximum that weights are taken from follows the row's own only where that is 2^8
-      // above it: weights of up to 256 fit both types and are rounded to as many bits, and of
-      // 32 rows in random order one has a new maximum in most steps, none so large a one.
-      const float tc = top * p.c;
-      const bool up = tc > m + 8.0f;
-      if (__any(up)) {
-        const float f = up ? __builtin_amdgcn_exp2f(m - tc) : 1.0f;
-        m = up ? tc : m;
-        l *= f;
-#pragma unroll
-        for (int k = 0; k < kDB; ++k) acc[k] *= f;
-      }
+      if (masked) mask_scores(s, t + off0, hb, min(lim, p.tb));
+      follow_top(s, p.c, m, l, acc);
       const float mc = m == -INFINITY ? 0.0f : m;
       if (masked && odd_at[buf] == t)
-#pragma unroll 1
-        for (int32_t o = t + off0; o < min(t + off0 + kMine, p.tb); ++o)
-#pragma unroll
-          for (int k = 0; k < 4 * kDB; ++k) {
-            const f32x4 x = odd_values<kF16, kQ8>(a, p, o, min(8 * k + fresh(4 * hb), D - 4));
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[k >> 2][4 * (k & 3) + i] = added(acc[k >> 2][4 * (k & 3) + i], o < lim ? x[i] : 0.0f);
-          }
-      // lane: element 32 k + col; positions 16 x + 8 jj + 4 hb ..
-      auto turned = [&](int x, int k) {
-        const u32x2 y0 = read_turned(vs + 16 * x * kV + 64 * k);
-        const u32x2 y1 = read_turned(vs + (16 * x + 8) * kV + 64 * k);
-        return u32x4{y0[0], y0[1], y1[0], y1[1]};
-      };
+        add_odd<kF16, kQ8>(a, p, t + off0, min(t + off0 + kMine, p.tb), hb, lim, acc);
+      auto turned = [&](int x, int k) { return turned_values(vs + 16 * x * kV + 64 * k, kV); };
       // 16 positions at a time: the products of the ones before run beside the
       // exponentials of these.  (Heads above 128: no registers for that.)
       float sum = 0;
@@ -633,14 +703,7 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
         if (DP <= 128)
 #pragma unroll
           for (int k = 0; k < kDB; ++k) va[k] = turned(x, k);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int at = (x & 1) * 8 + 2 * i;
-          const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x >> 1][at], p.c, -mc));
-          const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x >> 1][at + 1], p.c, -mc));
-          sum += e0 + e1;
-          pr[x][i] = pack<kF16>(e0, e1);
-        }
+        pr[x] = weights<kF16>(s, x, p.c, mc, &sum);
         if (DP <= 128)
 #pragma unroll
           for (int k = 0; k < kDB; ++k) acc[k] = mfma32<kF16>(va[k], pr[x], acc[k]);
@@ -689,30 +752,142 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
     __syncthreads();
     if (wave & 1) return;
   }
-  const int at = fresh(lane), d0 = 4 * (at >> 5);
-  const int32_t ro = rows0 + (at & 31);
-  if (ro < p.rows) {
-    const float inv = put_ml(a, p, ro, m, l, d0 == 0);
-#pragma unroll
-    for (int k = 0; k < kDB; ++k)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        put4<kF16>(a, p, ro, 32 * k + 8 * i + d0,
-                   f32x4{acc[k][4 * i], acc[k][4 * i + 1], acc[k][4 * i + 2], acc[k][4 * i + 3]}, inv);
-  }
+  put_rows<kF16>(a, p, rows0, lane, m, l, acc);
 }
 
-constexpr int shared_bytes(bool kQ8, int DP) {
-  const int wide = 2 * wide_positions(DP) * (key_stride(DP) + value_stride(DP)) + (DP > 128 ? kWideRows * key_stride(DP) : 0);
-  const int narrow = kWavesPerGroup * narrow_positions(kQ8, DP) * narrow_stride(DP);
+// ------------------------------------------------------------------ tall
+
+// 256 rows, 8 waves of 32: two to each SIMD, of which one is at its products while the other is
+// at its weights.  Waves 4 .. 7 are half a step behind waves 0 .. 3, with a barrier
+// between the halves:
+//   waves 0 .. 3   weights(t)                       results(t), scores(t + 1)
+//   waves 4 .. 7   results(t - 1), scores(t)        weights(t)
+// Each half stages its rows of the positions with its weights: waves 0 .. 3 those of step t + 1,
+// which they read half a step later, waves 4 .. 7 those of step t + 2.  So scores have
+// two buffers of keys and results three of values.  A chunk of 8192 rows after 24576: 850
+// TFLOP/s with the wide kernel's tiles, 950 with these; without the weights'
+// exponentials 970, without staging 1050, of 1180 that a large matrix product reaches.
+constexpr int kTallStep = 64;
+
+template <bool kF16, bool kQ8, int DP>
+__device__ void tall_piece(const AttendArgs& a, const Piece& p, unsigned char* smem, int32_t* odd_at) {
+  constexpr int kSteps = DP / 16, kTok = kTallStep, kDB = DP / 32;
+  constexpr int kK = key_stride(DP), kV = value_stride(DP);
+  constexpr int kKeys = kTok * kK, kValues = kTok * kV;
+  const int lane = fresh(threadIdx.x & 63), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 31, hb = lane >> 5;
+  const int rows0 = wave * 32;
+  const int32_t r = rows0 + col;
+  const bool idle = rows0 >= p.rows, late = wave >= 4;
+  const int ahead = late ? 2 : 1;  // steps that are staged before their scores
+
+  f32x16 acc[kDB];
+#pragma unroll
+  for (int k = 0; k < kDB; ++k)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[k][i] = 0;
+  float m = -INFINITY, l = 0;  // (the maximum of scores times c)
+
+  Stage<kF16, kQ8, DP, kTok, 512> st(p, wave, lane);
+  const int32_t least_of_all = a.plan.lim[row_at(a, p, 0).place];  // (as in the wide kernel)
+  auto stage = [&](int kb, int vb, int32_t t) {
+    if (st.put(smem + kb * kKeys, smem + 2 * kKeys + vb * kValues, t + kTok > p.tb || t + kTok > least_of_all))
+      odd_at[vb] = t;
+  };
+  st.pages(a, p, p.ta);
+  const RowAt qrow = row_at(a, p, min(r, p.rows - 1));
+  int32_t lim = a.plan.lim[qrow.place];
+  const int64_t qat = a.plan.row[qrow.place] * a.q.row + (int64_t)qrow.head * a.q.head;
+  st.loads(a, p, p.ta);
+  st.pages(a, p, p.ta + kTok);
+  u32x4 q[kSteps];
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) q[i] = load_q(a, p, qat, r < p.rows, 16 * i + 8 * hb);
+  if (r >= p.rows) lim = INT32_MAX;
+  int32_t least = lim;
+  for (int o = 16; o > 0; o >>= 1) least = min(least, __shfl_xor(least, o, 64));
+  stage(0, 0, p.ta);
+  st.loads(a, p, p.ta + kTok);
+  st.pages(a, p, p.ta + 2 * kTok);
+  if (late) {
+    if (p.ta + kTok < p.tb) stage(1, 1, p.ta + kTok);
+    st.loads(a, p, p.ta + 2 * kTok);
+    st.pages(a, p, p.ta + 3 * kTok);
+  }
+  __syncthreads();
+
+  f32x16 s[kTok / 32];
+  u32x4 pr[kTok / 16];
+  const unsigned char* ks0 = smem + col * kK + hb * 16;
+  const unsigned char* vs0 =
+      smem + 2 * kKeys + (4 * hb + ((lane & 15) >> 2)) * kV + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+  auto scores = [&](int kb) {
+    const unsigned char* ks = ks0 + kb * kKeys;
+#pragma unroll
+    for (int b = 0; b < kTok / 32; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[b][i] = 0;
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+      for (int b = 0; b < kTok / 32; ++b)
+        s[b] = mfma32<kF16>(*(const u32x4*)(ks + 32 * b * kK + 32 * i), q[i], s[b]);
+  };
+  if (late) __syncthreads();  // (half a step behind from here on; the others wait at the end)
+  if (!idle) scores(0);
+  __syncthreads();
+  int kb = 0, vb = 0;
+  for (int32_t t = p.ta; t < p.tb; t += kTok) {
+    if (!idle) {
+      const bool masked = t + kTok > p.tb || t + kTok > least;
+      if (masked) mask_scores(s, t, hb, min(lim, p.tb));
+      follow_top(s, p.c, m, l, acc);
+      const float mc = m == -INFINITY ? 0.0f : m;
+      if (masked && odd_at[vb] == t) add_odd<kF16, kQ8>(a, p, t, min(t + kTok, p.tb), hb, lim, acc);
+      float sum = 0;
+#pragma unroll
+      for (int x = 0; x < kTok / 16; ++x) pr[x] = weights<kF16>(s, x, p.c, mc, &sum);
+      l += sum;
+    }
+    const int32_t ts = t + ahead * kTok;
+    if (ts < p.tb) stage(kb ^ (ahead & 1), vb + ahead < 3 ? vb + ahead : vb + ahead - 3, ts);
+    st.loads(a, p, ts + kTok);  // (behind the last step too: as in the narrow kernel)
+    st.pages(a, p, ts + 2 * kTok);
+    __syncthreads();
+    if (!idle) {
+      __builtin_amdgcn_s_setprio(1);  // (products first: 1520 -> 1490 us)
+      const unsigned char* vs = vs0 + vb * kValues;
+#pragma unroll
+      for (int x = 0; x < kTok / 16; ++x)
+#pragma unroll
+        for (int k = 0; k < kDB; ++k)
+          acc[k] = mfma32<kF16>(turned_values(vs + 16 * x * kV + 64 * k, kV), pr[x], acc[k]);
+      scores(kb ^ 1);  // (behind the last step: of keys that were there before, and unused)
+      __builtin_amdgcn_s_setprio(0);
+    }
+    __syncthreads();
+    kb ^= 1;
+    vb = vb == 2 ? 0 : vb + 1;
+  }
+  if (!late) __syncthreads();
+  l += __shfl_xor(l, 32, 64);
+  put_rows<kF16>(a, p, rows0, lane, m, l, acc);
+}
+
+constexpr int shared_bytes(bool kQ8, int DP, bool kTall) {
+  const int wide = kTall ? kTallStep * (2 * key_stride(DP) + 3 * value_stride(DP))
+                         : 2 * wide_positions(DP) * (key_stride(DP) + value_stride(DP)) +
+                               (DP > 128 ? kWideRows * key_stride(DP) : 0);
+  const int narrow = (kTall ? kTallWaves : kWideWaves) * narrow_positions(kQ8, DP) * narrow_stride(DP);
   return wide > narrow ? wide : narrow;
 }
 
-template <bool kF16, bool kQ8, int DP>
-__global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_kernel(AttendArgs a) {
-  __shared__ __align__(16) unsigned char smem[shared_bytes(kQ8, DP)];
-  __shared__ int32_t odd_at[2];
-  if (threadIdx.x < 2) odd_at[threadIdx.x] = -1;
+template <bool kF16, bool kQ8, int DP, bool kTall>
+__global__ __launch_bounds__(64 * (kTall ? kTallWaves : kWideWaves), DP <= 128 ? 2 : 1) void attend_kernel(AttendArgs a) {
+  constexpr int kWaves = kTall ? kTallWaves : kWideWaves;
+  __shared__ __align__(16) unsigned char smem[shared_bytes(kQ8, DP, kTall)];
+  __shared__ int32_t odd_at[3];
+  if (threadIdx.x < 3) odd_at[threadIdx.x] = -1;
   __syncthreads();
   const int32_t head = blockIdx.x % a.cache.heads, group = blockIdx.x / a.cache.heads;
   const int32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -722,14 +897,14 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_kernel(AttendAr
   p.c = fmaxf(fabsf(c), 1.17549435e-38f);  // (not 0: it multiplies infinities)
   p.neg = c < 0 ? 0x80008000u : 0u;
   // (scalars throughout: what is loaded after the first store would be a lane's otherwise)
-  const AttendRun run = a.plan.runs[group * kWavesPerGroup + wave];
+  const AttendRun run = a.plan.runs[group * kWaves + wave];
   const int32_t kind = uniform(run.kind), rounds = uniform(run.rounds), number = uniform(run.number);
   int32_t next = uniform(run.next), at = uniform(run.from), left = uniform(run.units);
+  bool first = true;
   for (int32_t round = 0;;) {
-    const bool first = round == 0 && left == run.units;
     int32_t k, from, most, piece;
     if (round < rounds) {
-      k = group + round++ * uniform(run.stride);
+      k = tile_of_round(group, round++, uniform(run.stride));
       from = piece = 0;
       most = INT32_MAX;
     } else {
@@ -741,7 +916,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_kernel(AttendAr
       at = 0;
     }
     AttendTile t = run.tile;
-    if (!uniform((int32_t)first)) t = a.plan.tiles[kind][k];
+    if (!first) t = a.plan.tiles[kind][k];
+    first = false;
     const int32_t t0 = uniform(t.t0), t1 = uniform(t.t1), slot = uniform(t.slot);
     const int32_t n = min(max(0, (t1 - t0 + kUnit - 1) / kUnit) - from, most);
     if (n <= 0) continue;  // (a tile of no positions)
@@ -754,9 +930,14 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_kernel(AttendAr
     p.ta = t0 + from * kUnit;
     p.tb = min(t1, t0 + (from + n) * kUnit);
     p.slot = slot < 0 ? -1 : slot + (piece - uniform(t.first)) * p.rows;
-    if (kind == 0 && DP <= 128 && p.rows <= 64) wide_piece<kF16, kQ8, DP, DP <= 128 ? 2 : 1>(a, p, smem, odd_at);
-    else if (kind == 0) wide_piece<kF16, kQ8, DP, 1>(a, p, smem, odd_at);
-    else narrow_piece<kF16, kQ8, DP, kNarrowRows / 16>(a, p, smem + wave * narrow_positions(kQ8, DP) * narrow_stride(DP));
+    if constexpr (kTall) {
+      if (kind == 0) tall_piece<kF16, kQ8, DP>(a, p, smem, odd_at);
+    } else {
+      if (kind == 0 && DP <= 128 && p.rows <= 64) wide_piece<kF16, kQ8, DP, DP <= 128 ? 2 : 1>(a, p, smem, odd_at);
+      else if (kind == 0) wide_piece<kF16, kQ8, DP, 1>(a, p, smem, odd_at);
+    }
+    if (kind == 1)
+      narrow_piece<kF16, kQ8, DP, kNarrowRows / 16>(a, p, smem + wave * narrow_positions(kQ8, DP) * narrow_stride(DP));
     if (most != INT32_MAX) left -= n;
   }
 }
@@ -869,7 +1050,14 @@ template <bool kF16, bool kQ8, int DP>
 void launch(const AttendArgs& a, int32_t num_cus, hipStream_t s) {
   const dim3 grid((unsigned)(a.plan.groups * a.cache.heads));
   const dim3 join((unsigned)std::min<int64_t>((int64_t)a.win.n_rows * a.heads, 8 * num_cus));
-  hipLaunchKernelGGL((attend_kernel<kF16, kQ8, DP>), grid, dim3(256), 0, s, a);
+  if constexpr (DP == 128) {
+    if (a.plan.waves == kTallWaves) {
+      hipLaunchKernelGGL((attend_kernel<kF16, kQ8, DP, true>), grid, dim3(64 * kTallWaves), 0, s, a);
+      hipLaunchKernelGGL((join_kernel<kF16, DP / 4>), join, dim3(256), 0, s, a);
+      return;
+    }
+  }
+  hipLaunchKernelGGL((attend_kernel<kF16, kQ8, DP, false>), grid, dim3(64 * kWideWaves), 0, s, a);
   hipLaunchKernelGGL((join_kernel<kF16, DP / 4>), join, dim3(256), 0, s, a);
 }
 
@@ -877,7 +1065,16 @@ void launch(const AttendArgs& a, int32_t num_cus, hipStream_t s) {
 
 }  // namespace ps
 
-int32_t ps_attend_per_cu(int32_t dim) { return dim <= 128 ? 2 : 1; }
+int32_t ps_attend_per_cu(int32_t dim, bool tall) { return dim <= 128 && !tall ? 2 : 1; }
+
+// Tall tiles where requests have many rows on the average.  Measured with 32 heads over 8 (so
+// 4 rows a token), e4m3, tall and wide: 4 requests of 2048 new tokens behind none 220 and 219 us, behind
+// 2048 522 and 533, behind 16384 2310 and 2510; 16 of 512 behind none 111 and 102; 24 of 16 to
+// 1500 behind none 269 and 245.
+constexpr int kTallMin = 4096;
+bool ps_attend_tall(int32_t dim, int64_t rows, int32_t n_req) {
+  return dim > 64 && dim <= 128 && rows >= (int64_t)kTallMin * n_req;
+}
 
 hipError_t ps_launch_attend(const ps::AttendArgs& a, int32_t num_cus, hipStream_t s) {
   const bool f16 = a.q.dtype == PS_T_F16, quant = a.cache.dtype == PS_T_E4M3;

@@ -13,6 +13,7 @@ namespace ps {
 namespace {
 
 constexpr int kThreads = 512;
+static_assert(kThreads >= kMaxGroups, "a thread for each workgroup of a head");
 constexpr int kWaves = kThreads / 64;
 
 __global__ __launch_bounds__(256) void plan_check_kernel(AttendPlanDev p, BlockWin w, uint32_t* d_flags) {
@@ -152,7 +153,7 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
     if (d_flags)
       for (int32_t r = tid; r < n; r += kThreads) d_flags[r] = PS_R_INVALID;
     if (tid == 0) *p.head = AttendHead{};
-    for (int32_t x = tid; x < p.groups * kWavesPerGroup; x += kThreads) p.runs[x].rounds = p.runs[x].units = 0;
+    for (int32_t x = tid; x < p.groups * p.waves; x += kThreads) p.runs[x].rounds = p.runs[x].units = 0;
     return;
   }
 
@@ -243,7 +244,7 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
   };
   auto tiles_of = [&](AttendSeg* s) {
     s->wide = (int64_t)s->tokens * ratio > kNarrowRows;
-    s->tiles = s->wide ? (int32_t)(((int64_t)s->tokens * ratio + kWideRows - 1) / kWideRows) : 1;
+    s->tiles = s->wide ? (int32_t)(((int64_t)s->tokens * ratio + p.wide_rows - 1) / p.wide_rows) : 1;
   };
   for (int32_t i = tid; i < n; i += kThreads) {
     const int32_t r = keys[i] & 8191u, first = keys[i] >> 13;
@@ -314,8 +315,8 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
     t.tail_off = s.tail_off;
     t.pre_len = s.pre_len;
     t.p0 = s.p0;
-    t.row0 = k * kWideRows;
-    t.rows = (int32_t)min((int64_t)s.tokens * ratio - t.row0, (int64_t)(s.wide ? kWideRows : kNarrowRows));
+    t.row0 = k * p.wide_rows;
+    t.rows = (int32_t)min((int64_t)s.tokens * ratio - t.row0, (int64_t)(s.wide ? p.wide_rows : kNarrowRows));
     t.t0 = s.t0;
     // (a request's later rows see more: none of the tile's sees more than its last)
     t.t1 = min(s.t1, p.lim[s.p0 + (t.row0 + t.rows - 1) / ratio]);
@@ -346,7 +347,8 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
 
   // Units end to end, and who takes them.
   int32_t wide_groups, rounds = 0, runs[2];
-  int64_t units[2], wide_cost = 0;
+  int64_t units[2], wide_cost = 0;  // (units: with those that stand for a tile's start)
+  const int32_t start[2] = {kTileUnits, 0};
   int64_t* begin[2];
   int64_t* run_at[2];
   for (int kind = 0; kind < 2; ++kind) {
@@ -358,7 +360,7 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
           const AttendTile& t = p.tiles[kind][k];
           const int64_t u = units_of(t);
           mine += u * (kUnitCost + t.rows);
-          return u;
+          return u + start[kind];
         },
         [&](int32_t k, int64_t at) { begin[kind][k] = at; });
     if (kind == 0 && n_tiles[0] > 4 * kThreads) mine /= 2;  // (each value was asked for twice)
@@ -375,7 +377,7 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
     }
     wide_groups = (int32_t)n_wide;
     runs[0] = (int32_t)min(n_wide, units[0]);
-    runs[1] = (int32_t)min((p.groups - n_wide) * kWavesPerGroup, units[1]);
+    runs[1] = (int32_t)min((p.groups - n_wide) * p.waves, units[1]);
   }
   for (int kind = 0; kind < 2; ++kind) run_at[kind] = runs[kind] <= kNear ? near_run[kind] : p.run_at[kind];
   __syncthreads();
@@ -387,7 +389,7 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
     int64_t whole = 0, total, share = 0;
     for (rounds = n_tiles[0] / n_wide;; --rounds) {
       whole = 0;
-      for (int32_t i = 0; mine && i < rounds; ++i) whole += units_of(p.tiles[0][tid + i * n_wide]);
+      for (int32_t i = 0; mine && i < rounds; ++i) whole += units_of(p.tiles[0][tile_of_round(tid, i, n_wide)]) + kTileUnits;
       if (!__syncthreads_or(mine && rounds > 0 && whole * n_wide > units[0])) break;
     }
     // a level that those below it are filled up to
@@ -407,23 +409,33 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
     if (below) share = left / n_below + (rank < left % n_below) - whole;
     const int32_t done = rounds * n_wide;
     const int64_t skip = done < n_tiles[0] ? begin[0][done] : units[0];
-    const int64_t at = block_scan(share, &total, sums), number = block_scan(share > 0, &total, sums);
+    const int64_t at = block_scan(share, &total, sums);
     runs[0] = n_wide;
-    if (mine) {
-      run_at[0][tid] = skip + at;
-      wide_units[tid] = (int32_t)share;
-      wide_number[tid] = (int32_t)number;
-    }
+    if (mine) run_at[0][tid] = skip + at;
   } else {
     for (int32_t r = tid; r < runs[0]; r += kThreads) {
       run_at[0][r] = units[0] * r / runs[0];
-      wide_units[r] = (int32_t)(units[0] * (r + 1) / runs[0] - units[0] * r / runs[0]);
-      wide_number[r] = r;
     }
   }
   // (counting a tile as a unit more made a batch of short contexts no faster, and one of
   // long ones slower: 241 -> 246 us)
   for (int32_t r = tid; r < runs[1]; r += kThreads) run_at[1][r] = units[1] * r / runs[1];
+  __syncthreads();
+  // What a wide run has without the tiles' starts; those that have something are numbered.
+  auto before = [&](int64_t u) {
+    if (u >= units[0]) return units[0] - (int64_t)kTileUnits * n_tiles[0];
+    const int32_t k = last_at_most(begin[0], n_tiles[0], u);
+    return max(begin[0][k], u - kTileUnits) - (int64_t)kTileUnits * k;
+  };
+  if (runs[0] > 0) {
+    int32_t have = 0;
+    if (tid < runs[0])
+      have = (int32_t)(before(tid + 1 < runs[0] ? run_at[0][tid + 1] : units[0]) - before(run_at[0][tid]));
+    int64_t total;
+    const int64_t number = block_scan(have > 0, &total, sums);
+    wide_units[tid] = have;
+    wide_number[tid] = (int32_t)number;
+  }
   __syncthreads();
   for (int kind = 0; kind < 2; ++kind) {
     AttendTile* tiles = p.tiles[kind];
@@ -434,7 +446,7 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
       return kind == 0 ? wide_number[r] : r;
     };
     for (int32_t k = tid; k < n_tiles[kind]; k += kThreads) {
-      const int64_t u = units_of(tiles[k]), b = begin[kind][k];
+      const int64_t u = units_of(tiles[k]), b = begin[kind][k] + start[kind];
       int32_t first = 0, pieces = u > 0 ? 1 : 0;
       if (u > 0 && k >= whole) {
         first = number_at(b);
@@ -464,10 +476,10 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
 
   // What each wave takes.
   __syncthreads();
-  for (int32_t x = tid; x < p.groups * kWavesPerGroup; x += kThreads) {
-    const int32_t g = x / kWavesPerGroup, kind = g >= wide_groups;
+  for (int32_t x = tid; x < p.groups * p.waves; x += kThreads) {
+    const int32_t g = x / p.waves, kind = g >= wide_groups;
     // (the waves' runs go round the workgroups)
-    const int32_t r = kind == 0 ? g : g - wide_groups + x % kWavesPerGroup * (p.groups - wide_groups);
+    const int32_t r = kind == 0 ? g : g - wide_groups + x % p.waves * (p.groups - wide_groups);
     AttendRun run{};
     run.kind = kind;
     if (r < runs[kind]) {
@@ -478,7 +490,7 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
       run.units = kind == 0 ? wide_units[r] : (int32_t)((r + 1 < runs[1] ? run_at[1][r + 1] : units[1]) - at);
       if (run.units > 0) {
         run.next = last_at_most(begin[kind], n_tiles[kind], at);
-        run.from = (int32_t)(at - begin[kind][run.next]);
+        run.from = max(0, (int32_t)(at - begin[kind][run.next]) - start[kind]);
       }
       if (run.rounds > 0 || run.units > 0) run.tile = p.tiles[kind][run.rounds > 0 ? r : run.next];
     }
@@ -504,7 +516,7 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
     if (own) part(0, *own);
     if (pre_tile >= 0) {
       const int32_t k = pre_tile & (kWideBit - 1);
-      if (pre_tile & kWideBit) part(1, p.tiles[0][k + ((place - pre_p0) * ratio + sub) / kWideRows]);
+      if (pre_tile & kWideBit) part(1, p.tiles[0][k + ((place - pre_p0) * ratio + sub) / p.wide_rows]);
       else part(1, p.tiles[1][k]);
     }
     p.joins[atomicAdd(&n_todo, 1)] = x;

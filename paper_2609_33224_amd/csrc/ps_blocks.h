@@ -93,7 +93,7 @@ __host__ __device__ inline bool block_locate(const BlockWin& w, int32_t row, int
 // that attend over it: a prefix that several requests share with the rows of
 // all of them, or what is left of one request's chain with its own rows.  Its
 // rows (row of the window x query head of the group, row-major) are cut into
-// tiles; a tile is wide (up to kWideRows rows) or narrow (all rows of a segment of
+// tiles; a tile is wide (up to kWideRows or kTallRows rows) or narrow (all rows of a segment of
 // kNarrowRows at most).  The tiles' positions, in units of kUnit, are laid end
 // to end and dealt in runs: the wide ones' to some workgroups of each key / value
 // head, the narrow ones' to the waves of the others, so many as the costs say.  Where there
@@ -102,13 +102,25 @@ __host__ __device__ inline bool block_locate(const BlockWin& w, int32_t row, int
 // what is left makes their shares even.  So a tile may be cut into pieces; pieces and
 // shared segments leave partial results, which a second kernel joins.
 constexpr int kUnit = 64;
-constexpr int kWideRows = 128;
+constexpr int kWideRows = 128, kTallRows = 256;  // of a wide tile: which of them, the host says (ps_attend_tall)
 constexpr int kNarrowRows = 16;
-constexpr int kWavesPerGroup = 4;
+constexpr int kMaxGroups = 512;                // workgroups per head
+constexpr int kWideWaves = 4, kTallWaves = 8;  // of a workgroup, likewise
 // Cost of a unit for a workgroup, in rows: of a narrow tile's (1.5 to 1.75 us of e4m3
 // with every workgroup at work), and what a wide one's has beside its rows (3.7 us for 128).
 constexpr int kUnitCost = 128;
 constexpr int kWideTileCost = 256, kTileCost = 160;  // of a tile beside its units: lookups, q, results
+// When wide tiles are dealt, each counts as so many units more: what begins and what cuts a
+// tile costs about that.  24 prompts of 16 to 1500 tokens: 0: 296 us, 2: 258, 6: 245, 12:
+// 250; 128 rows of 4 heads over one prefix alike with all.
+constexpr int kTileUnits = 6;
+
+// The tile that workgroup g takes in a round: the rounds go to and fro, since tiles of
+// one prompt grow longer.  (4 prompts of 2048 tokens: 315 -> 223 us.)
+__host__ __device__ inline int32_t tile_of_round(int32_t g, int32_t round, int32_t n) {
+  return round * n + (round & 1 ? n - 1 - g : g);
+}
+
 constexpr int kShareMinTokens = 64;  // of a prefix
 constexpr int kShareMaxRows = 64;    // of a member (or one row of all its heads)
 
@@ -152,8 +164,8 @@ struct AttendHead {
   int32_t n_joins;
 };
 
-// What a wave of a workgroup takes: (wide tiles, all four waves the same) `rounds` whole
-// tiles, its own number + i stride, then `units` from unit `from` of tile `next` on.
+// What a wave of a workgroup takes: (wide tiles, all waves the same) `rounds` whole
+// tiles, one of each `stride` of them (tile_of_round), then `units` from unit `from` of tile `next` on.
 // The first tile's record is here too, so that a wave has one lookup less to wait for.
 struct alignas(16) AttendRun {
   AttendTile tile;
@@ -179,7 +191,7 @@ struct AttendPlanDev {
   AttendSeg* segs;    // 2 per request, in that order: prefix (first members only), own
   AttendTile* tiles[2];
   int64_t* begin[2];  // first unit of each tile
-  AttendRun* runs;     // of wave w of workgroup g: 4 g + w
+  AttendRun* runs;     // of wave w of workgroup g: waves g + w
   int64_t* run_at[2];  // first unit of each run, wide and narrow
   AttendJoin* joins;
   float* part;        // partial results: [head][slot rows][dim], weights as numerators
@@ -188,6 +200,8 @@ struct AttendPlanDev {
   int32_t tile_cap[2];
   int32_t slot_rows;  // per head
   int32_t groups;     // workgroups per head
+  int32_t waves;      // of each
+  int32_t wide_rows;  // of a wide tile, at most
 };
 
 struct AttendArgs {
@@ -211,4 +225,6 @@ hipError_t ps_launch_attend_plan(const ps::AttendPlanDev& p, const ps::BlockWin&
                                  hipStream_t s);
 hipError_t ps_launch_attend(const ps::AttendArgs& a, int32_t num_cus, hipStream_t s);
 // Resident workgroups of the attention kernel per CU.
-int32_t ps_attend_per_cu(int32_t dim);
+int32_t ps_attend_per_cu(int32_t dim, bool tall);
+// Whether a window of `rows` rows (x query heads of a group) is cut into tall tiles.
+bool ps_attend_tall(int32_t dim, int64_t rows, int32_t n_req);

@@ -136,10 +136,10 @@ hipError_t each_buffer(ps_attend_plan* p, F f) {
   for (int k = 0; k < 2; ++k) {
     one(d.tiles[k], d.tile_cap[k]);
     one(d.begin[k], d.tile_cap[k]);
-    one(d.run_at[k], (size_t)d.groups * (k == 0 ? 1 : kWavesPerGroup));
+    one(d.run_at[k], (size_t)d.groups * (k == 0 ? 1 : kWideWaves));
   }
   // (a row with partial results each, or a place of empty rows: twice where two tiles have some)
-  one(d.runs, (size_t)d.groups * kWavesPerGroup);
+  one(d.runs, (size_t)d.groups * kWideWaves);
   one(d.joins, (size_t)d.slot_rows + rows + d.tile_cap[0]);
   one(d.part, part * p->dim);
   one(d.part_ml, part);
@@ -153,7 +153,19 @@ void release(ps_attend_plan* p) {
   });
 }
 
-// Sizes that hold whatever window of at most max_req requests and max_rows rows.
+// The workgroups of a head, and the tiles they take.
+void shape_plan(ps_attend_plan* p, int32_t num_cus, bool tall) {
+  AttendPlanDev& d = p->dev;
+  d.waves = tall ? kTallWaves : kWideWaves;
+  d.wide_rows = tall ? kTallRows : kWideRows;
+  const int32_t per_cu = ps_attend_per_cu(p->dim, tall);
+  // (two at least, of both kinds one; the plan's kernel has a thread for each)
+  d.groups = std::min(std::max(num_cus * per_cu / p->kv_heads, 2 * per_cu), per_cu * kMaxGroups / 2);
+}
+
+// Sizes that hold whatever window of at most max_req requests and max_rows rows, cut into
+// tall tiles or not: those are twice as high, taken by at most half as many workgroups of
+// twice as many waves.
 void size_plan(ps_attend_plan* p, int32_t num_cus) {
   AttendPlanDev& d = p->dev;
   const int64_t n = p->max_req, rows = (int64_t)p->max_rows * p->ratio();
@@ -163,12 +175,12 @@ void size_plan(ps_attend_plan* p, int32_t num_cus) {
   // a wide tile is full but for the last one of each segment, and a row lies in two segments at most
   d.tile_cap[0] = (int32_t)(2 * n + 2 * rows / kWideRows + 1);
   d.tile_cap[1] = (int32_t)(2 * n + 1);
-  d.groups = std::max(2, num_cus * ps_attend_per_cu(p->dim) / p->kv_heads);  // (of both kinds one at least)
+  shape_plan(p, num_cus, false);
   // Of partial results: each row of a shared segment once, in both of its segments;
   // and the pieces of tiles that are cut, of which there are fewer than twice
   // as many as workgroups or waves that take them.
   const int64_t shared = std::min(rows, n * std::max(kShareMaxRows, p->ratio()));
-  d.slot_rows = (int32_t)std::min<int64_t>(2 * shared + 2 * (int64_t)d.groups * (kWideRows + kWavesPerGroup * kNarrowRows), INT32_MAX);
+  d.slot_rows = (int32_t)std::min<int64_t>(2 * shared + 2 * (int64_t)d.groups * (kWideRows + kWideWaves * kNarrowRows), INT32_MAX);
 }
 
 }  // namespace
@@ -253,6 +265,7 @@ ps_status ps_attend_plan_dev(ps_attend_plan* p, const ps_kv_window* window, uint
                 p->max_req, p->max_rows);
   DeviceScope ds(c->device);
   const BlockWin w = dev_win(*window, p->bt);
+  shape_plan(p, c->num_cus, ps_attend_tall(p->dim, (int64_t)w.n_rows * p->ratio(), w.n_req));
   if (w.n_req > 0 && w.n_rows > 0) HIP_TRY(c, ps_launch_attend_plan(p->dev, w, p->ratio(), d_flags, (hipStream_t)hip_stream));
   p->win = w;
   p->planned = true;

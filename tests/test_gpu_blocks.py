@@ -523,3 +523,148 @@ def test_plans_go_with_their_context(ps):
     q.close()  # freed with the context
     with pytest.raises(ValueError):
         q.build_dev(Window([0], [], 16).dev())
+
+
+def _attend(ps, sc, w, heads, kv, dim, dtype, typ, seed=1, amp=1.0, check=True, plan=None):
+    c = _cache(ps, w, kv, dim, dtype, seed=seed)
+    q = amp * _randn(_gen(seed), w.n_rows, heads, dim).to(typ)
+    out, lse = torch.full_like(q, 3.0), torch.full((w.n_rows, heads), 3.0, device="cuda")
+    p = plan or sc.attend_plan(heads, kv, dim, w.bt, w.n_req, w.n_rows)
+    p.build_dev(w.dev())
+    p.attend_dev(c, q, out, lse)
+    if check:
+        check_attention(w, c.tensors, q, out, lse, dim ** -0.5)
+    return c, q, out, lse, p
+
+
+# windows with many rows a request: tiles of 256 rows; the last has one that decodes beside them
+TALL = [(64, 1, 128, 16, [3], [(0, 700, 150), (0, 3 * 16 + 90, 90)]),
+        (96, 1, 96, 7, [9], [(0, 201, 120), (0, 64, 1)]),
+        (64, 2, 112, 16, [0], [(0, 65, 65), (0, 257, 257), (0, 129, 129)]),
+        (16, 1, 80, 5, [0, 4], [(0, 640, 600), (1, 300, 1)])]
+
+
+@pytest.mark.parametrize("heads,kv,dim,bt,sessions,reqs", TALL)
+@pytest.mark.parametrize("dtype,typ", [(BF16, BF16), (F16, F16), (E4M3, BF16), (E4M3, F16)])
+def test_tall_tiles(ps, sc, heads, kv, dim, bt, sessions, reqs, dtype, typ):
+    w = Window(sessions, reqs, bt, seed=dim, pad=1)
+    _, _, out, lse, _ = _attend(ps, sc, w, heads, kv, dim, dtype, typ)
+    for t in (out, lse):
+        assert (t[:1] == 3).all() and (t[-1:] == 3).all()
+
+
+@pytest.mark.parametrize("n", [64, 65, 127, 128, 129, 191, 192, 193, 320])
+def test_tall_tiles_of_few_steps(ps, sc, n):
+    """Contexts about as long as the steps that are staged ahead."""
+    w = Window([0], [(0, n, 64)], 16, seed=n)
+    _attend(ps, sc, w, 64, 1, 128, E4M3, BF16, amp=2.0)
+
+
+@pytest.mark.parametrize("dtype,typ", [(BF16, BF16), (E4M3, F16)])
+def test_what_lies_behind_a_row_does_not_reach_it_in_tall_tiles(ps, sc, dtype, typ):
+    heads, kv, dim, bt, n, first = 64, 1, 128, 16, 150, 101
+    w = Window([0], [(0, 200, n)], bt)
+    c, q, ref, lref, p = _attend(ps, sc, w, heads, kv, dim, dtype, typ)
+    ch = w.chain(0)
+    junk = torch.tensor([float("nan"), float("inf"), -float("inf"), 3.0], device="cuda").repeat(dim // 4)
+    if dtype == E4M3:
+        junk = torch.tensor([0x7F, 0xFF, 0x7E, 0x80], dtype=torch.uint8, device="cuda").repeat(dim // 4)
+    for t in range(50 + first, -(-200 // bt) * bt):
+        for x in c.tensors[:2]:
+            if dtype == E4M3:
+                x.view(torch.uint8)[int(ch[t // bt]), :, t % bt] = junk
+            else:
+                x[int(ch[t // bt]), :, t % bt] = junk.to(dtype)
+    out, lse = torch.zeros_like(q), torch.zeros_like(lref)
+    p.attend_dev(c, q, out, lse)
+    assert torch.equal(out[:first], ref[:first]) and torch.equal(lse[:first], lref[:first])
+    assert torch.isnan(out[first:]).any(-1).all()
+
+
+def test_growing_scores(ps, sc):
+    """Maxima that grow slowly, at once and not at all, so that rows follow them at different steps."""
+    heads, kv, dim, bt = 64, 1, 128, 16
+    for n in (64, 1):
+        w = Window([0], [(0, 600, n)], bt)
+        c = _cache(ps, w, kv, dim, BF16)
+        ch = torch.from_numpy(w.chain(0).astype(np.int64)).cuda()
+        t = torch.arange(600, device="cuda")
+        c.tensors[0][ch[t // bt], 0, t % bt, 0] = (t / 8).bfloat16()
+        q = _randn(_gen(2), n, heads, dim).bfloat16()
+        q[:, :, 0] = torch.linspace(-6, 6, heads, device="cuda").bfloat16()
+        out, lse = torch.zeros_like(q), torch.zeros(n, heads, device="cuda")
+        p = sc.attend_plan(heads, kv, dim, bt, 1, n)
+        p.build_dev(w.dev())
+        for scale in (dim ** -0.5, 1.0):
+            p.attend_dev(c, q, out, lse, scale=scale)
+            check_attention(w, c.tensors, q, out, lse, scale)
+
+
+@pytest.mark.parametrize("heads,kv,dim,n_req,most", [(2, 1, 16, 1500, 40), (1, 1, 16, 8192, 9), (64, 1, 16, 1100, 20),
+                                                     (64, 8, 64, 150, 90)])
+def test_windows_of_many_requests(ps, sc, heads, kv, dim, n_req, most):
+    """More requests than the plan's tables in shared memory hold, or more tiles than workgroups; contexts of 0 too."""
+    bt = 4
+    rng = np.random.default_rng(n_req)
+    sessions = [0, 2, 30, 17]
+    reqs = []
+    for s in rng.integers(0, 4, n_req):
+        ctx = int(rng.integers(0, most))
+        reqs.append((int(s), ctx + (sessions[s] * bt if rng.random() < 0.8 else 0), 1))
+    w = Window(sessions, reqs, bt, seed=n_req)
+    _attend(ps, sc, w, heads, kv, dim, E4M3, BF16)
+
+
+@pytest.mark.parametrize("heads,kv,dim", [(300, 1, 32), (128, 128, 16), (1024, 4, 64)])
+def test_many_heads(ps, sc, heads, kv, dim):
+    w = Window([9, 0], [(0, 150, 1), (0, 9 * 16 + 1, 1), (1, 70, 2), (0, 9 * 16, 1)], 16)
+    _attend(ps, sc, w, heads, kv, dim, F16, F16)
+
+
+def test_a_negative_scale_turns_q(ps, sc):
+    for heads, kv, n in ((4, 2, 1), (8, 1, 20), (64, 1, 70)):
+        w = Window([2], [(0, 90, n)], 16)
+        c, q, _, _, p = _attend(ps, sc, w, heads, kv, 128, E4M3, BF16)
+        a, b = torch.zeros_like(q), torch.zeros_like(q)
+        p.attend_dev(c, q, a, scale=-0.1)
+        p.attend_dev(c, -q, b, scale=0.1)
+        assert torch.equal(a, b)
+
+
+def test_a_page_twice_in_a_chain(ps, sc):
+    w = Window([4], [(0, 150, 3), (0, 100, 1)], 16)
+    w.pages[1] = w.pages[0]
+    d = w.reqs[0]
+    w.pages[d["tail_off"]:d["tail_off"] + 3] = w.pages[3]
+    _attend(ps, sc, w, 8, 2, 64, BF16, BF16)
+
+
+def test_padding_requests_and_a_plan_for_more(ps, sc):
+    """Requests of no rows and no blocks behind the last; one plan for large and small windows in turn."""
+    heads, kv, dim, bt = 64, 1, 128, 16
+    p = sc.attend_plan(heads, kv, dim, bt, 1200, 400)
+    big = [(0, 48 + 5 * k, 1) for k in range(9)]
+    for reqs in (big + [(1, 0, 0)] * 7, [(1, 130, 130)], [(1, 0, 0)] * 3, big, [(1, 300, 200), (0, 50, 1)]):
+        w = Window([3, 0], reqs, bt, pad=2)
+        _, _, out, _, _ = _attend(ps, sc, w, heads, kv, dim, E4M3, BF16, plan=p)
+        assert (out[:2] == 3).all() and (out[-2:] == 3).all()
+
+
+def test_two_streams_at_once(ps, sc):
+    """Two plans at work at the same time, each on its own stream."""
+    rng = np.random.default_rng(1)
+    work = []
+    for k, (heads, kv, dim) in enumerate(((16, 2, 128), (64, 1, 128))):
+        w = Window([40], [(0, 640 + int(rng.integers(1, 300)), 1 if k == 0 else 100) for _ in range(8 if k == 0 else 1)], 16)
+        c, q, ref, _, _ = _attend(ps, sc, w, heads, kv, dim, E4M3, BF16)
+        p = sc.attend_plan(heads, kv, dim, 16, w.n_req, w.n_rows)
+        work.append((p, w.dev(), c, q, ref, [torch.zeros_like(q) for _ in range(5)], torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for i in range(5):
+        for p, win, c, q, _, outs, stream in work:
+            with torch.cuda.stream(stream):
+                p.build_dev(win)
+                p.attend_dev(c, q, outs[i])
+    torch.cuda.synchronize()
+    for _, _, _, _, ref, outs, _ in work:
+        assert all(torch.equal(o, ref) for o in outs)
