@@ -543,7 +543,9 @@ ps_status ps_kv_read_dev(ps_ctx* ctx, const ps_kv_cache* cache, const ps_kv_wind
  * for it (from the context; freed by ps_attend_plan_destroy, or with the
  * context).  It serves windows of at most max_req requests and max_rows rows
  * with n_heads query heads over n_kv_heads (a divisor of n_heads) and the
- * given head_dim and block_tokens.
+ * given head_dim and block_tokens.  A plan is destroyed, or its context is,
+ * once the work that uses it is done and no graph that holds it will run
+ * again: its memory goes to the context's next buffers.
  */
 typedef struct ps_attend_plan ps_attend_plan;
 ps_status ps_attend_plan_create(ps_ctx* ctx, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
@@ -556,9 +558,10 @@ ps_status ps_attend_plan_destroy(ps_attend_plan* plan);
  * pages (which may change afterwards only if the plan is made again; page
  * numbers are read again by the attention).  Requests with the same pre_off
  * and pre_len share one pass over that segment's keys and values where it
- * pays.  d_flags[n_req] (may be NULL) receives 0, or PS_R_INVALID for a request whose segments leave the pool, whose
- * chain is longer than PS_MAX_CHAIN blocks, whose ctx_tok is negative, more
- * than the chain holds or above PS_MAX_WINDOW_CTX, or that needs a page outside [0, n_pages); its rows
+ * pays.  d_flags[n_req] (may be NULL) receives 0, or PS_R_INVALID for a
+ * request whose segments leave the pool, whose chain is longer than
+ * PS_MAX_CHAIN blocks, whose ctx_tok is negative, more than the chain holds or
+ * above PS_MAX_WINDOW_CTX, or that needs a page outside [0, n_pages); its rows
  * come out as empty ones.  Where row_off is not ascending within [0, n_rows],
  * every request is flagged and the attention writes nothing.  One plan serves
  * every layer of a step.  No allocation: it can be captured, and a replay

@@ -379,7 +379,7 @@ class KvCache:
                         or x.stride() != k_exp.stride() or (x.numel() and x.stride()[1:] != (block, 1))):
                     raise ValueError("k_exp and v_exp must be uint8 (pages, KV heads, block tokens), "
                                      "a page contiguous")
-            stride = max(k_exp.stride(0), heads * block)
+            stride = k_exp.stride(0) if pages > 1 else heads * block  # (one page has no stride that matters)
         elif any(x is not None for x in exps):
             raise ValueError("exponents belong to float8_e4m3fn caches")
         self.tensors = (k, v, k_exp, v_exp)
@@ -387,7 +387,7 @@ class KvCache:
         self.shape = (heads, dim)
         self.dtype = k.dtype
         self.raw = PsKvCache(k.data_ptr(), v.data_ptr(), *[x.data_ptr() if x is not None else None for x in exps],
-                             pages, max(k.stride(0), heads * block * dim), stride, heads, dim, block,
+                             pages, k.stride(0) if pages > 1 else heads * block * dim, stride, heads, dim, block,
                              types[k.dtype])
 
     @classmethod
@@ -508,6 +508,7 @@ class AttendPlan:
         if d_flags is not None and (d_flags.element_size() != 4 or d_flags.numel() < window.n_req):
             raise ValueError("d_flags must hold 32 bits per request")
         _same_device(window.device, d_flags)
+        self.scorer._check_device(window.device)
         _check(self.scorer.ctx, load_library().ps_attend_plan_dev(
             self._handle(), ctypes.byref(window.raw), _dev_ptr(d_flags), _block_stream(stream, window.device)))
         self.window = window
@@ -553,6 +554,7 @@ class Scorer:
 
     def __init__(self, device: int = 0):
         self.ctx = ps_create(device)
+        self.device_index = int(device)
         self.n_inst = 0
 
     def close(self):
@@ -624,10 +626,16 @@ class Scorer:
     def replay_dev(self, d_pool, pool_len, d_reqs, n_req, d_inst, d_out, stream=None) -> int:
         return ps_replay_window_dev(self.ctx, d_pool, pool_len, d_reqs, n_req, d_inst, d_out, stream)
 
+    def _check_device(self, device: torch.device) -> None:
+        if device.index != self.device_index:
+            raise ValueError(f"tensors on {device}, the context is on device {self.device_index}")
+
     def kv_write_dev(self, cache: KvCache, window: KvWindow, k, v, stream=None) -> None:
+        self._check_device(cache.device)
         ps_kv_write_dev(self.ctx, cache, window, k, v, stream)
 
     def kv_read_dev(self, cache: KvCache, window: KvWindow, k, v, stream=None) -> None:
+        self._check_device(cache.device)
         ps_kv_read_dev(self.ctx, cache, window, k, v, stream)
 
     def attend_plan(self, n_heads: int, n_kv_heads: int, head_dim: int, block_tokens: int, max_req: int,

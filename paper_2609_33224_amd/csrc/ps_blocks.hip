@@ -8,7 +8,6 @@
 #include "ps_blocks.h"
 #include "ps_context.h"
 
-
 struct ps_attend_plan {
   ps_ctx* ctx = nullptr;
   ps_attend_plan* next = nullptr;
@@ -265,8 +264,9 @@ ps_status ps_attend_plan_dev(ps_attend_plan* p, const ps_kv_window* window, uint
                 p->max_req, p->max_rows);
   DeviceScope ds(c->device);
   const BlockWin w = dev_win(*window, p->bt);
+  p->planned = false;  // (until the launches have succeeded)
   shape_plan(p, c->num_cus, ps_attend_tall(p->dim, (int64_t)w.n_rows * p->ratio(), w.n_req));
-  if (w.n_req > 0 && w.n_rows > 0) HIP_TRY(c, ps_launch_attend_plan(p->dev, w, p->ratio(), d_flags, (hipStream_t)hip_stream));
+  if (w.n_req > 0) HIP_TRY(c, ps_launch_attend_plan(p->dev, w, p->ratio(), d_flags, (hipStream_t)hip_stream));
   p->win = w;
   p->planned = true;
   return PS_OK;

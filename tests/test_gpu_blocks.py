@@ -668,3 +668,40 @@ def test_two_streams_at_once(ps, sc):
     torch.cuda.synchronize()
     for _, _, _, _, ref, outs, _ in work:
         assert all(torch.equal(o, ref) for o in outs)
+
+
+def test_flags_of_a_window_without_rows(ps, sc):
+    w = Window([2], [(0, 40, 0), (0, 0, 0), (0, 35, 0)], 16)
+    w.reqs[2]["pre_off"] = 1 << 40
+    flags = torch.full((3,), 9, dtype=torch.int32, device="cuda")
+    p = sc.attend_plan(4, 2, 64, 16, 3, 0)
+    p.build_dev(w.dev(), d_flags=flags)
+    assert w.n_rows == 0 and flags.tolist() == [0, 0, 8]
+    c = _cache(ps, w, 2, 64, E4M3)
+    q = torch.ones(1, 4, 64, dtype=BF16, device="cuda")
+    p.attend_dev(c, q, q)
+    assert (q == 1).all()
+
+
+def test_pages_over_each_other_and_other_devices_are_refused(ps, sc):
+    w = Window([0], [(0, 20, 2)], 16)
+    win, rows = w.dev(), torch.zeros(2, 1, 64, dtype=BF16, device="cuda")
+    one = ps.KvCache.empty(1, 1, 16, 64)
+    k, v, kx, vx = one.tensors
+    n = w.n_pages
+    for c in (ps.KvCache(k.expand(n, -1, -1, -1), v.expand(n, -1, -1, -1), *(x.repeat(n, 1, 1) for x in (kx, vx))),
+              ps.KvCache(k.repeat(n, 1, 1, 1), v.repeat(n, 1, 1, 1), *(x.expand(n, -1, -1) for x in (kx, vx)))):
+        for call in (sc.kv_write_dev, sc.kv_read_dev):
+            with pytest.raises(ps.PackServeError) as e:
+                call(c, win, rows, rows)
+            assert e.value.code == ps.binding.PS_E_INVAL and "stride" in str(e.value)
+    c = ps.KvCache.empty(n, 1, 16, 64)
+    p = sc.attend_plan(1, 1, 64, 16, 1, 2)
+    sc.device_index += 1
+    try:
+        for call in (lambda: sc.kv_write_dev(c, win, rows, rows), lambda: sc.kv_read_dev(c, win, rows, rows),
+                     lambda: p.build_dev(win)):
+            with pytest.raises(ValueError):
+                call()
+    finally:
+        sc.device_index -= 1
