@@ -21,6 +21,11 @@
 //    take turns with the matrix cores.
 // e4m3 values are brought to the 16-bit type with their power of two as they
 // are staged (exact but for fp16's range), so one kernel serves both.
+//
+// Scores, maxima, sums and results are in fp32 throughout.  Two things are rounded to the
+// 16-bit type: the weights, which the second product takes in it (each by half a step at
+// most, 2^-8 of its own size in bf16 and 2^-11 in fp16, so a result by no more than that of
+// sum p |v|; the sum that divides them takes them as they were), and the result.
 
 #include <algorithm>
 
@@ -154,11 +159,18 @@ struct Spot {
 };
 // (A page number was checked when the plan was made; one that has changed since is
 // kept inside the cache.)
-__device__ inline Spot spot_of(const AttendArgs& a, int32_t head, uint32_t page, int32_t t) {
+__device__ inline Spot spot_at(const AttendArgs& a, int32_t head, uint32_t page, uint32_t slot) {
   page = min(page, (uint32_t)a.cache.n_pages - 1u);
-  const int32_t slot = t - block_of(a, t) * a.win.bt;
-  const int32_t r = head * a.win.bt + slot;
-  return Spot{(int64_t)page * a.cache.page_stride + (int64_t)r * a.cache.dim, (int64_t)page * a.cache.exp_stride + r};
+  const uint32_t r = (uint32_t)(head * a.win.bt) + slot;  // (r dim < 2^32: the limits of heads, blocks and dim)
+  const uint64_t row = r * (uint32_t)a.cache.dim;
+  // (a product of 64 bits is three of 32, and strides of pages that need it are rare)
+  uint64_t at = (uint64_t)page * (uint32_t)a.cache.page_stride + row, x = (uint64_t)page * (uint32_t)a.cache.exp_stride + r;
+  if (a.cache.page_stride >> 32) at += (uint64_t)(page * (uint32_t)(a.cache.page_stride >> 32)) << 32;
+  if (a.cache.exp_stride >> 32) x += (uint64_t)(page * (uint32_t)(a.cache.exp_stride >> 32)) << 32;
+  return Spot{(int64_t)at, (int64_t)x};
+}
+__device__ inline Spot spot_of(const AttendArgs& a, int32_t head, uint32_t page, int32_t t) {
+  return spot_at(a, head, page, (uint32_t)(t - block_of(a, t) * a.win.bt));
 }
 
 // One piece of a tile: positions [ta, tb) for its rows.
@@ -476,17 +488,19 @@ struct Stage {
   static constexpr int kChunk = kQ8 ? 32 : 16;                     // bytes in shared memory of such a load
   const int row, sc;  // thread x: row x / kPer, chunks x % kPer + kPer i
   const int32_t last;
-  uint32_t page;
+  uint32_t page, slot;
   u32x4 kr[kLoads], vr[kLoads];
   uint32_t kx = 0, vx = 0;
 
   __device__ Stage(const Piece& p, int wave, int lane)
       : row(wave * (64 / kPer) + lane / kPer), sc(lane % kPer), last(p.tb - 1) {}
   __device__ void pages(const AttendArgs& a, const Piece& p, int32_t t) {
-    page = page_of(a, p.chain, min(t + row, last));
+    const int32_t at = min(t + row, last), b = block_of(a, at);
+    slot = (uint32_t)(at - b * a.win.bt);
+    page = (uint32_t)(b < p.chain.pre_len ? p.chain.pre : p.chain.tail)[b];
   }
-  __device__ void loads(const AttendArgs& a, const Piece& p, int32_t t) {
-    const Spot s = spot_of(a, p.head, page, min(t + row, last));
+  __device__ void loads(const AttendArgs& a, const Piece& p) {
+    const Spot s = spot_at(a, p.head, page, slot);
     const int D = a.cache.dim;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
@@ -530,6 +544,14 @@ struct Stage {
   }
 };
 
+// The larger of a lane's value and that of the lane 32 from it.
+__device__ inline float max_of_halves(float x) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(u, u, false, false));
+  const uint32_t own = y[0], other = y[1];  // (a bit cast of y[1] itself reads y[0]: the compiler's)
+  return fmaxf(__builtin_bit_cast(float, own), __builtin_bit_cast(float, other));
+}
+
 // A wave's scores of 32 kB positions from t, lane: position 32 b + 8 (i / 4) + 4 hb + i % 4:
 // those that the row does not see are taken out.
 template <int kB>
@@ -550,7 +572,7 @@ __device__ inline void follow_top(const f32x16 (&s)[kB], float c, float& m, floa
   float top = s[0][0];
 #pragma unroll
   for (int i = 1; i < 16 * kB; ++i) top = fmaxf(top, s[i >> 4][i & 15]);
-  top = fmaxf(top, __shfl_xor(top, 32, 64));
+  top = max_of_halves(top);
   const float tc = top * c;
   const bool up = tc > m + 8.0f;
   if (__any(up)) {
@@ -651,7 +673,7 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
   const RowAt qrow = row_at(a, p, min(r, p.rows - 1));
   int32_t lim = a.plan.lim[qrow.place];
   const int64_t qat = a.plan.row[qrow.place] * a.q.row + (int64_t)qrow.head * a.q.head;
-  st.loads(a, p, p.ta);
+  st.loads(a, p);
   st.pages(a, p, p.ta + kTok);
   // (heads above 128: no registers for q, it stays in shared memory)
   u32x4 q[DP <= 128 ? kSteps : 1];
@@ -669,7 +691,7 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
   __syncthreads();
   int buf = 0;
   for (int32_t t = p.ta; t < p.tb; t += kTok, buf ^= 1) {
-    st.loads(a, p, t + kTok);  // (behind the last step too: as in the narrow kernel)
+    st.loads(a, p);  // (behind the last step too: as in the narrow kernel)
     st.pages(a, p, t + 2 * kTok);
     if (!idle) {
       const unsigned char* ks = smem + buf * kTile + (off0 + col) * kK + hb * 16;
@@ -764,9 +786,12 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
 //   waves 4 .. 7   results(t - 1), scores(t)        weights(t)
 // Each half stages its rows of the positions with its weights: waves 0 .. 3 those of step t + 1,
 // which they read half a step later, waves 4 .. 7 those of step t + 2.  So scores have
-// two buffers of keys and results three of values.  A chunk of 8192 rows after 24576: 850
-// TFLOP/s with the wide kernel's tiles, 950 with these; without the weights'
-// exponentials 970, without staging 1050, of 1180 that a large matrix product reaches.
+// two buffers of keys and results three of values.  In the products, operands are read
+// four products ahead of their use (2100 cycles with the reads where the compiler puts
+// them, 1300 so; the weights take 1400 and staging 700).
+//
+// Chunks of 777 to 2048 tokens behind 8192 to 16384, 32 heads over 8: 850 TFLOP/s with the
+// wide kernel's tiles, 990 to 1030 with these, of 1180 that a large matrix product reaches.
 constexpr int kTallStep = 64;
 
 template <bool kF16, bool kQ8, int DP>
@@ -774,11 +799,12 @@ __device__ void tall_piece(const AttendArgs& a, const Piece& p, unsigned char* s
   constexpr int kSteps = DP / 16, kTok = kTallStep, kDB = DP / 32;
   constexpr int kK = key_stride(DP), kV = value_stride(DP);
   constexpr int kKeys = kTok * kK, kValues = kTok * kV;
+  static_assert(DP == 128 && kTok == 64, "four products of results and of scores at a time");
   const int lane = fresh(threadIdx.x & 63), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, hb = lane >> 5;
   const int rows0 = wave * 32;
   const int32_t r = rows0 + col;
-  const bool idle = rows0 >= p.rows, late = wave >= 4;
+  const bool late = wave >= 4;
   const int ahead = late ? 2 : 1;  // steps that are staged before their scores
 
   f32x16 acc[kDB];
@@ -798,7 +824,7 @@ __device__ void tall_piece(const AttendArgs& a, const Piece& p, unsigned char* s
   const RowAt qrow = row_at(a, p, min(r, p.rows - 1));
   int32_t lim = a.plan.lim[qrow.place];
   const int64_t qat = a.plan.row[qrow.place] * a.q.row + (int64_t)qrow.head * a.q.head;
-  st.loads(a, p, p.ta);
+  st.loads(a, p);
   st.pages(a, p, p.ta + kTok);
   u32x4 q[kSteps];
 #pragma unroll
@@ -807,63 +833,81 @@ __device__ void tall_piece(const AttendArgs& a, const Piece& p, unsigned char* s
   int32_t least = lim;
   for (int o = 16; o > 0; o >>= 1) least = min(least, __shfl_xor(least, o, 64));
   stage(0, 0, p.ta);
-  st.loads(a, p, p.ta + kTok);
+  st.loads(a, p);
   st.pages(a, p, p.ta + 2 * kTok);
   if (late) {
-    if (p.ta + kTok < p.tb) stage(1, 1, p.ta + kTok);
-    st.loads(a, p, p.ta + 2 * kTok);
+    stage(1, 1, p.ta + kTok);  // (behind the last step, its last position over: as in the narrow kernel)
+    st.loads(a, p);
     st.pages(a, p, p.ta + 3 * kTok);
   }
   __syncthreads();
 
-  f32x16 s[kTok / 32];
+  f32x16 s[2];
   u32x4 pr[kTok / 16];
   const unsigned char* ks0 = smem + col * kK + hb * 16;
   const unsigned char* vs0 =
       smem + 2 * kKeys + (4 * hb + ((lane & 15) >> 2)) * kV + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
-  auto scores = [&](int kb) {
-    const unsigned char* ks = ks0 + kb * kKeys;
+  // the four operands of a round of products: values of 16 positions, keys of 64 and 32 elements
+  auto values = [&](u32x4 (&x)[4], const unsigned char* vs, int i) {
 #pragma unroll
-    for (int b = 0; b < kTok / 32; ++b)
+    for (int k = 0; k < 4; ++k) x[k] = turned_values(vs + 16 * i * kV + 64 * k, kV);
+  };
+  auto keys = [&](u32x4 (&x)[4], const unsigned char* ks, int i) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[b][i] = 0;
+    for (int k = 0; k < 4; ++k) x[k] = *(const u32x4*)(ks + 32 * (k & 1) * kK + 32 * (2 * i + (k >> 1)));
+  };
+  auto scores = [&](const u32x4 (&x)[4], int i) {
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i)
+    for (int k = 0; k < 4; ++k) {
+      if (i == 0 && k < 2)
 #pragma unroll
-      for (int b = 0; b < kTok / 32; ++b)
-        s[b] = mfma32<kF16>(*(const u32x4*)(ks + 32 * b * kK + 32 * i), q[i], s[b]);
+        for (int e = 0; e < 16; ++e) s[k][e] = 0;
+      s[k & 1] = mfma32<kF16>(x[k], q[2 * i + (k >> 1)], s[k & 1]);
+    }
   };
   if (late) __syncthreads();  // (half a step behind from here on; the others wait at the end)
-  if (!idle) scores(0);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    u32x4 x[4];
+    keys(x, ks0, i);
+    scores(x, i);
+  }
   __syncthreads();
   int kb = 0, vb = 0;
   for (int32_t t = p.ta; t < p.tb; t += kTok) {
-    if (!idle) {
-      const bool masked = t + kTok > p.tb || t + kTok > least;
-      if (masked) mask_scores(s, t, hb, min(lim, p.tb));
-      follow_top(s, p.c, m, l, acc);
-      const float mc = m == -INFINITY ? 0.0f : m;
-      if (masked && odd_at[vb] == t) add_odd<kF16, kQ8>(a, p, t, min(t + kTok, p.tb), hb, lim, acc);
-      float sum = 0;
+    const bool masked = t + kTok > p.tb || t + kTok > least;
+    if (masked) mask_scores(s, t, hb, min(lim, p.tb));
+    follow_top(s, p.c, m, l, acc);
+    const float mc = m == -INFINITY ? 0.0f : m;
+    if (masked && odd_at[vb] == t) add_odd<kF16, kQ8>(a, p, t, min(t + kTok, p.tb), hb, lim, acc);
+    float sum = 0;
 #pragma unroll
-      for (int x = 0; x < kTok / 16; ++x) pr[x] = weights<kF16>(s, x, p.c, mc, &sum);
-      l += sum;
+    for (int x = 0; x < kTok / 16; ++x) pr[x] = weights<kF16>(s, x, p.c, mc, &sum);
+    l += sum;
+    {
+      const int v2 = vb + ahead;
+      stage(kb ^ (ahead & 1), v2 < 3 ? v2 : v2 - 3, t + ahead * kTok);
     }
-    const int32_t ts = t + ahead * kTok;
-    if (ts < p.tb) stage(kb ^ (ahead & 1), vb + ahead < 3 ? vb + ahead : vb + ahead - 3, ts);
-    st.loads(a, p, ts + kTok);  // (behind the last step too: as in the narrow kernel)
-    st.pages(a, p, ts + 2 * kTok);
+    st.loads(a, p);
+    st.pages(a, p, t + (ahead + 2) * kTok);
     __syncthreads();
-    if (!idle) {
-      __builtin_amdgcn_s_setprio(1);  // (products first: 1520 -> 1490 us)
-      const unsigned char* vs = vs0 + vb * kValues;
+
+    const unsigned char *vs = vs0 + vb * kValues, *ks = ks0 + (kb ^ 1) * kKeys;
+    // (behind the last step: scores of keys that were there before, unused)
+    u32x4 x[2][4];
+    values(x[0], vs, 0);
 #pragma unroll
-      for (int x = 0; x < kTok / 16; ++x)
+    for (int i = 0; i < 8; ++i) {
+      if (i < 3) values(x[(i + 1) & 1], vs, i + 1);
+      else if (i < 7) keys(x[(i + 1) & 1], ks, i - 3);
+      __builtin_amdgcn_sched_barrier(0);
+      if (i < 4) {
 #pragma unroll
-        for (int k = 0; k < kDB; ++k)
-          acc[k] = mfma32<kF16>(turned_values(vs + 16 * x * kV + 64 * k, kV), pr[x], acc[k]);
-      scores(kb ^ 1);  // (behind the last step: of keys that were there before, and unused)
-      __builtin_amdgcn_s_setprio(0);
+        for (int k = 0; k < 4; ++k) acc[k] = mfma32<kF16>(x[i & 1][k], pr[i], acc[k]);
+      } else {
+        scores(x[i & 1], i - 4);
+      }
+      __builtin_amdgcn_sched_barrier(0);
     }
     __syncthreads();
     kb ^= 1;
@@ -1067,11 +1111,12 @@ void launch(const AttendArgs& a, int32_t num_cus, hipStream_t s) {
 
 int32_t ps_attend_per_cu(int32_t dim, bool tall) { return dim <= 128 && !tall ? 2 : 1; }
 
-// Tall tiles where requests have many rows on the average.  Measured with 32 heads over 8 (so
-// 4 rows a token), e4m3, tall and wide: 4 requests of 2048 new tokens behind none 220 and 219 us, behind
-// 2048 522 and 533, behind 16384 2310 and 2510; 16 of 512 behind none 111 and 102; 24 of 16 to
-// 1500 behind none 269 and 245.
-constexpr int kTallMin = 4096;
+// Tall tiles where requests have many rows on the average.  They gain where much lies behind the
+// rows and lose a little where nothing does, which only the device knows.  Measured with 32 heads over
+// 8 (4 rows a token), e4m3, wide and tall: 8 requests of 700 new tokens behind 16384 1785 and 1580
+// us, 4 of 512 706 and 626; 4 of 2048 behind 2048 540 and 491, behind none 220 and 212; 16 of 512
+// behind none 102 and 111, 24 of 16 to 1500 249 and 263.  (8 heads over 8: 8 of 512 behind 16384 362 and 320.)
+constexpr int kTallMin = 1024;
 bool ps_attend_tall(int32_t dim, int64_t rows, int32_t n_req) {
   return dim > 64 && dim <= 128 && rows >= (int64_t)kTallMin * n_req;
 }

@@ -705,3 +705,22 @@ def test_pages_over_each_other_and_other_devices_are_refused(ps, sc):
                 call()
     finally:
         sc.device_index -= 1
+
+
+def test_growing_scores_in_half_precision(ps, sc):
+    """Weights are taken from a maximum that may lie 2^8 below the row's: they must stay in the type's range."""
+    heads, kv, dim, bt = 64, 1, 128, 16
+    for n in (64, 1):
+        w = Window([0], [(0, 600, n)], bt)
+        c = _cache(ps, w, kv, dim, F16)
+        ch = torch.from_numpy(w.chain(0).astype(np.int64)).cuda()
+        t = torch.arange(600, device="cuda")
+        c.tensors[0][ch[t // bt], 0, t % bt, 0] = ((t * 37) % 600 / 8).half()
+        q = _randn(_gen(2), n, heads, dim).half()
+        q[:, :, 0] = torch.linspace(-6, 6, heads, device="cuda").half()
+        out, lse = torch.zeros_like(q), torch.zeros(n, heads, device="cuda")
+        p = sc.attend_plan(heads, kv, dim, bt, 1, n)
+        p.build_dev(w.dev())
+        for scale in (dim ** -0.5, 1.0):
+            p.attend_dev(c, q, out, lse, scale=scale)
+            check_attention(w, c.tensors, q, out, lse, scale)
