@@ -563,25 +563,27 @@ __device__ inline void mask_scores(f32x16 (&s)[kB], int32_t t, int hb, int32_t e
       if (t + 32 * b + 8 * (i >> 2) + 4 * hb + (i & 3) >= end) s[b][i] = -INFINITY;
 }
 
-// The running maximum (m, of scores times c) after these scores; the sum and the results follow it.
-// It follows the row's own only where that is 2^8 above it: weights of up to 256 fit both
-// types and are rounded to as many bits, and of 32 rows in random order one has a new
-// maximum in most steps, none so large a one.
-template <int kB, int kDB>
-__device__ inline void follow_top(const f32x16 (&s)[kB], float c, float& m, float& l, f32x16 (&acc)[kDB]) {
+// The largest of a row's scores, times c.
+template <int kB>
+__device__ inline float top_of(const f32x16 (&s)[kB], float c) {
   float top = s[0][0];
 #pragma unroll
   for (int i = 1; i < 16 * kB; ++i) top = fmaxf(top, s[i >> 4][i & 15]);
-  top = max_of_halves(top);
-  const float tc = top * c;
-  const bool up = tc > m + 8.0f;
-  if (__any(up)) {
-    const float f = up ? __builtin_amdgcn_exp2f(m - tc) : 1.0f;
-    m = up ? tc : m;
-    l *= f;
+  return max_of_halves(top) * c;
+}
+
+// The running maximum (m, of scores times c) of the rows that say so becomes top; the sum and the results
+// follow it.  It need not be the row's own: rows say so where that is 2^8 above it or more. Weights of
+// some hundreds fit both types and are rounded to as many bits, and of 32 rows in random
+// order one has a new maximum in most steps, none so large a one.  (Whether a row says so depends on
+// the row alone, so its bits do not depend on what lies beside it.)
+template <int kDB>
+__device__ inline void raise_top(bool up, float top, float& m, float& l, f32x16 (&acc)[kDB]) {
+  const float f = up ? __builtin_amdgcn_exp2f(m - top) : 1.0f;
+  m = up ? top : m;
+  l *= f;
 #pragma unroll
-    for (int k = 0; k < kDB; ++k) acc[k] *= f;
-  }
+  for (int k = 0; k < kDB; ++k) acc[k] *= f;
 }
 
 // The infinities and NaN that were taken out of positions [t, end)'s values, to the rows that see them.
@@ -661,10 +663,10 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
 
   Stage<kF16, kQ8, DP, kTok, 256> st(p, wave, lane);
   // (of one request's rows the first sees least; those of a shared prefix see all of it)
-  const int32_t least_of_all = a.plan.lim[row_at(a, p, 0).place];
+  const int32_t least_of_all = min(uniform(a.plan.lim[row_at(a, p, 0).place]), p.tb);
   auto stage = [&](int buf, int32_t t) {
     unsigned char* keys = smem + buf * kTile;
-    if (st.put(keys, keys + kKeys, t + kTok > p.tb || t + kTok > least_of_all))
+    if (st.put(keys, keys + kKeys, t + kTok > least_of_all))
       odd_at[buf] = t;  // (a value left by another piece only costs a look)
   };
 
@@ -710,9 +712,12 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
       }
       const bool masked = t + kTok > p.tb || t + kTok > least;
       if (masked) mask_scores(s, t + off0, hb, min(lim, p.tb));
-      follow_top(s, p.c, m, l, acc);
+      const float top = top_of(s, p.c);
+      const bool up = top > m + 8.0f;
+      if (__any(up)) raise_top(up, top, m, l, acc);
       const float mc = m == -INFINITY ? 0.0f : m;
-      if (masked && odd_at[buf] == t)
+      // (also for a wave whose rows all see all of the step)
+      if (t + kTok > least_of_all && odd_at[buf] == t)
         add_odd<kF16, kQ8>(a, p, t + off0, min(t + off0 + kMine, p.tb), hb, lim, acc);
       auto turned = [&](int x, int k) { return turned_values(vs + 16 * x * kV + 64 * k, kV); };
       // 16 positions at a time: the products of the ones before run beside the
@@ -815,9 +820,9 @@ __device__ void tall_piece(const AttendArgs& a, const Piece& p, unsigned char* s
   float m = -INFINITY, l = 0;  // (the maximum of scores times c)
 
   Stage<kF16, kQ8, DP, kTok, 512> st(p, wave, lane);
-  const int32_t least_of_all = a.plan.lim[row_at(a, p, 0).place];  // (as in the wide kernel)
+  const int32_t least_of_all = min(uniform(a.plan.lim[row_at(a, p, 0).place]), p.tb);  // (as in the wide kernel)
   auto stage = [&](int kb, int vb, int32_t t) {
-    if (st.put(smem + kb * kKeys, smem + 2 * kKeys + vb * kValues, t + kTok > p.tb || t + kTok > least_of_all))
+    if (st.put(smem + kb * kKeys, smem + 2 * kKeys + vb * kValues, t + kTok > least_of_all))
       odd_at[vb] = t;
   };
   st.pages(a, p, p.ta);
@@ -877,12 +882,29 @@ __device__ void tall_piece(const AttendArgs& a, const Piece& p, unsigned char* s
   for (int32_t t = p.ta; t < p.tb; t += kTok) {
     const bool masked = t + kTok > p.tb || t + kTok > least;
     if (masked) mask_scores(s, t, hb, min(lim, p.tb));
-    follow_top(s, p.c, m, l, acc);
-    const float mc = m == -INFINITY ? 0.0f : m;
-    if (masked && odd_at[vb] == t) add_odd<kF16, kQ8>(a, p, t, min(t + kTok, p.tb), hb, lim, acc);
-    float sum = 0;
+    if (t + kTok > least_of_all && odd_at[vb] == t) {
+      // (rows without a maximum take theirs first: their results are multiplied by 0 then)
+      const float top = top_of(s, p.c);
+      raise_top(m == -INFINITY && top > m, top, m, l, acc);
+      add_odd<kF16, kQ8>(a, p, t, min(t + kTok, p.tb), hb, lim, acc);
+    }
+    // Weights from the maximum as it is, which is nearly always near enough.  The row's own is
+    // looked for where there is none yet, or where a lane's 32 weights sum up to 2^13,
+    // so that one of them is 2^8 at least (and none leaves fp16).
+    auto all_weights = [&] {
+      const float mc = m == -INFINITY ? 0.0f : m;
+      float sum = 0;
 #pragma unroll
-    for (int x = 0; x < kTok / 16; ++x) pr[x] = weights<kF16>(s, x, p.c, mc, &sum);
+      for (int x = 0; x < kTok / 16; ++x) pr[x] = weights<kF16>(s, x, p.c, mc, &sum);
+      return sum;
+    };
+    float sum = all_weights();
+    const uint64_t far = __ballot(sum > 8192.0f || m == -INFINITY);
+    if (far) {
+      const float top = top_of(s, p.c);
+      raise_top((far | far >> 32) >> col & 1 && top > m, top, m, l, acc);
+      sum = all_weights();
+    }
     l += sum;
     {
       const int v2 = vb + ahead;

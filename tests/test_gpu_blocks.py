@@ -724,3 +724,20 @@ def test_growing_scores_in_half_precision(ps, sc):
         for scale in (dim ** -0.5, 1.0):
             p.attend_dev(c, q, out, lse, scale=scale)
             check_attention(w, c.tensors, q, out, lse, scale)
+
+
+@pytest.mark.parametrize("heads,n", [(4, 1), (4, 30), (64, 64)])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_an_infinity_that_is_seen(ps, sc, heads, n, dtype):
+    """Of one sign: every row that sees it is infinite in that element, the rows before it keep their bits."""
+    kv, dim, bt, ctx = 1, 128, 16, 64
+    w = Window([0], [(0, ctx, n)], bt)
+    c, q, ref, lref, p = _attend(ps, sc, w, heads, kv, dim, dtype, dtype)
+    at = ctx - 1 - n // 2
+    c.tensors[1][int(w.chain(0)[at // bt]), 0, at % bt, 5] = float("inf")
+    out, lse = torch.zeros_like(q), torch.zeros_like(lref)
+    p.attend_dev(c, q, out, lse)
+    sees = torch.arange(ctx - n, ctx, device="cuda") >= at
+    assert torch.equal(lse, lref) and torch.equal(out[~sees], ref[~sees])
+    rest = torch.arange(dim, device="cuda") != 5
+    assert (out[sees][:, :, 5] == float("inf")).all() and torch.equal(out[:, :, rest], ref[:, :, rest])
