@@ -793,10 +793,10 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
 // which they read half a step later, waves 4 .. 7 those of step t + 2.  So scores have
 // two buffers of keys and results three of values.  In the products, operands are read
 // four products ahead of their use (2100 cycles with the reads where the compiler puts
-// them, 1300 so; the weights take 1400 and staging 700).
+// them, 1300 so; the weights took 1400 with a maximum looked for in every step, staging 700).
 //
 // Chunks of 777 to 2048 tokens behind 8192 to 16384, 32 heads over 8: 850 TFLOP/s with the
-// wide kernel's tiles, 990 to 1030 with these, of 1180 that a large matrix product reaches.
+// wide kernel's tiles, 1060 to 1090 with these, of 1180 that a large matrix product reaches.
 constexpr int kTallStep = 64;
 
 template <bool kF16, bool kQ8, int DP>
@@ -1135,9 +1135,9 @@ int32_t ps_attend_per_cu(int32_t dim, bool tall) { return dim <= 128 && !tall ? 
 
 // Tall tiles where requests have many rows on the average.  They gain where much lies behind the
 // rows and lose a little where nothing does, which only the device knows.  Measured with 32 heads over
-// 8 (4 rows a token), e4m3, wide and tall: 8 requests of 700 new tokens behind 16384 1785 and 1580
-// us, 4 of 512 706 and 626; 4 of 2048 behind 2048 540 and 491, behind none 220 and 212; 16 of 512
-// behind none 102 and 111, 24 of 16 to 1500 249 and 263.  (8 heads over 8: 8 of 512 behind 16384 362 and 320.)
+// 8 (4 rows a token), e4m3, wide and tall: 8 requests of 700 new tokens behind 16384 1728 and 1451
+// us, 4 of 512 702 and 581; 4 of 2048 behind 2048 536 and 461, behind none 222 and 206; 16 of 512
+// behind none 101 and 114, 24 of 16 to 1500 244 and 259.  (8 heads over 8: 8 of 512 behind 16384 355 and 296.)
 constexpr int kTallMin = 1024;
 bool ps_attend_tall(int32_t dim, int64_t rows, int32_t n_req) {
   return dim > 64 && dim <= 128 && rows >= (int64_t)kTallMin * n_req;
