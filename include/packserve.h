@@ -585,7 +585,9 @@ ps_status ps_attend_plan_dev(ps_attend_plan* plan, const ps_kv_window* window, u
  * Asynchronous on `hip_stream`, no allocation.  The plan's memory is in use
  * until the work is done: calls on one plan must not overlap (two graphs that
  * may run at the same time need a plan each).  PS_E_STATE before
- * ps_attend_plan_dev.
+ * ps_attend_plan_dev.  Captured without its plan, it is for windows of the
+ * n_req, n_rows and buffers that were planned when it was captured; another
+ * window that is planned in between may leave out as it was.
  */
 ps_status ps_attend_window_dev(ps_attend_plan* plan, const ps_kv_cache* cache, const ps_rows* q,
                                const ps_rows* out, float* lse, float scale, void* hip_stream);

@@ -966,6 +966,8 @@ __global__ __launch_bounds__(64 * (kTall ? kTallWaves : kWideWaves), DP <= 128 ?
   const AttendRun run = a.plan.runs[group * kWaves + wave];
   const int32_t kind = uniform(run.kind), rounds = uniform(run.rounds), number = uniform(run.number);
   int32_t next = uniform(run.next), at = uniform(run.from), left = uniform(run.units);
+  // (a plan for workgroups of another size: the window planned last was not this launch's)
+  if (uniform(run.waves) != kWaves) return;
   bool first = true;
   for (int32_t round = 0;;) {
     int32_t k, from, most, piece;
@@ -1022,7 +1024,9 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
   const int lane = threadIdx.x & 63, sub = lane / LG, d = 4 * (lane % LG);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int32_t D = a.cache.dim;
-  const int64_t n = (int64_t)a.plan.head->n_joins * a.cache.heads;
+  const AttendHead plan = *a.plan.head;
+  if (plan.waves != a.plan.waves) return;  // (as in the attention kernel)
+  const int64_t n = (int64_t)plan.n_joins * a.cache.heads;
   const bool together = n <= gridDim.x;  // (the same for the grid)
   const int64_t first = together ? blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
   for (int64_t id = first; id < n; id += (int64_t)gridDim.x * (together ? 1 : 4)) {

@@ -152,8 +152,8 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
   if (__syncthreads_or(bad)) {
     if (d_flags)
       for (int32_t r = tid; r < n; r += kThreads) d_flags[r] = PS_R_INVALID;
-    if (tid == 0) *p.head = AttendHead{};
-    for (int32_t x = tid; x < p.groups * p.waves; x += kThreads) p.runs[x].rounds = p.runs[x].units = 0;
+    if (tid == 0) *p.head = AttendHead{0, p.waves};
+    for (int32_t x = tid; x < p.n_runs; x += kThreads) p.runs[x].rounds = p.runs[x].units = 0;
     return;
   }
 
@@ -476,13 +476,14 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
 
   // What each wave takes.
   __syncthreads();
-  for (int32_t x = tid; x < p.groups * p.waves; x += kThreads) {
+  for (int32_t x = tid; x < p.n_runs; x += kThreads) {
     const int32_t g = x / p.waves, kind = g >= wide_groups;
     // (the waves' runs go round the workgroups)
     const int32_t r = kind == 0 ? g : g - wide_groups + x % p.waves * (p.groups - wide_groups);
     AttendRun run{};
     run.kind = kind;
-    if (r < runs[kind]) {
+    run.waves = p.waves;
+    if (g < p.groups && r < runs[kind]) {
       run.rounds = kind == 0 ? rounds : 0;
       run.stride = wide_groups;
       run.number = kind == 0 ? wide_number[r] : r;
@@ -550,7 +551,7 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
         push(s.p0 + j, -1, nullptr, -1, 0);
   }
   __syncthreads();
-  if (tid == 0) *p.head = AttendHead{n_todo};
+  if (tid == 0) *p.head = AttendHead{n_todo, p.waves};
 }
 
 }  // namespace

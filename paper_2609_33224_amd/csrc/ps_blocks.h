@@ -162,6 +162,7 @@ struct alignas(16) AttendJoin {
 
 struct AttendHead {
   int32_t n_joins;
+  int32_t waves;  // AttendPlanDev::waves when the plan was made
 };
 
 // What a wave of a workgroup takes: (wide tiles, all waves the same) `rounds` whole
@@ -171,9 +172,10 @@ struct alignas(16) AttendRun {
   AttendTile tile;
   int32_t number;  // of the runs of its kind that have units
   int32_t kind;    // 0: wide, 1: narrow
+  int32_t waves;   // AttendHead::waves
   int32_t rounds, stride;
   int32_t next, from, units;
-  int32_t pad[3];
+  int32_t pad[2];
 };
 
 struct AttendPlanDev {
@@ -200,6 +202,7 @@ struct AttendPlanDev {
   int32_t tile_cap[2];
   int32_t slot_rows;  // per head
   int32_t groups;     // workgroups per head
+  int32_t n_runs;     // records of runs, at least groups * waves
   int32_t waves;      // of each
   int32_t wide_rows;  // of a wide tile, at most
 };

@@ -138,7 +138,7 @@ hipError_t each_buffer(ps_attend_plan* p, F f) {
     one(d.run_at[k], (size_t)d.groups * (k == 0 ? 1 : kWideWaves));
   }
   // (a row with partial results each, or a place of empty rows: twice where two tiles have some)
-  one(d.runs, (size_t)d.groups * kWideWaves);
+  one(d.runs, d.n_runs);
   one(d.joins, (size_t)d.slot_rows + rows + d.tile_cap[0]);
   one(d.part, part * p->dim);
   one(d.part_ml, part);
@@ -175,6 +175,7 @@ void size_plan(ps_attend_plan* p, int32_t num_cus) {
   d.tile_cap[0] = (int32_t)(2 * n + 2 * rows / kWideRows + 1);
   d.tile_cap[1] = (int32_t)(2 * n + 1);
   shape_plan(p, num_cus, false);
+  d.n_runs = d.groups * d.waves;
   // Of partial results: each row of a shared segment once, in both of its segments;
   // and the pieces of tiles that are cut, of which there are fewer than twice
   // as many as workgroups or waves that take them.

@@ -741,3 +741,30 @@ def test_an_infinity_that_is_seen(ps, sc, heads, n, dtype):
     assert torch.equal(lse, lref) and torch.equal(out[~sees], ref[~sees])
     rest = torch.arange(dim, device="cuda") != 5
     assert (out[sees][:, :, 5] == float("inf")).all() and torch.equal(out[:, :, rest], ref[:, :, rest])
+
+
+def test_attention_captured_without_its_plan(ps, sc):
+    """Another window planned in between, cut for other workgroups: nothing is written; the first one again: its
+    results."""
+    heads, kv, dim, bt = 63, 7, 128, 16
+    w = Window([2], [(0, 32 + 9 * k, 1) for k in range(12)], bt)
+    big = Window([0], [(0, 200, 190)], bt)
+    p = sc.attend_plan(heads, kv, dim, bt, 12, 190)
+    c, q, ref, _, _ = _attend(ps, sc, w, heads, kv, dim, E4M3, BF16, plan=p)
+    win, many = w.dev(), big.dev()
+    out = torch.full_like(q, 3.0)
+    p.build_dev(win)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        p.attend_dev(c, q, out)
+    for _ in range(3):
+        out.fill_(3.0)
+        p.build_dev(many)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert (out == 3).all()
+        p.build_dev(win)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, ref)
