@@ -14,6 +14,7 @@ namespace {
 
 constexpr int kThreads = 512;
 static_assert(kThreads >= kMaxGroups, "a thread for each workgroup of a head");
+static_assert(kTallWaves <= 2 * kWideWaves, "tall tiles: half as many workgroups");
 constexpr int kWaves = kThreads / 64;
 
 __global__ __launch_bounds__(256) void plan_check_kernel(AttendPlanDev p, BlockWin w, uint32_t* d_flags) {
@@ -109,14 +110,15 @@ __device__ inline int32_t last_at_most(const int64_t* v, int32_t n, int64_t u) {
 }
 
 constexpr int kSmall = 1024;  // requests, up to which the tables lie in shared memory
-constexpr int kNear = 1024;   // tiles and runs of a kind, likewise
+constexpr int kNear = 1024;   // tiles of a kind, likewise
 
 __device__ inline int64_t units_of(const AttendTile& t) { return (max(0, t.t1 - t.t0) + kUnit - 1) / kUnit; }
 
 // The steps: groups of requests with one prefix; the order of requests (groups
 // together) and of their rows; segments; tiles; units and runs; partial results and
 // what is to be joined.  Each ends with a barrier, of which the kernel's time is made:
-// 13 us for one request, 21 us for 128 in 24 groups.
+// 12 to 17 us for one request, 25 to 29 us for 128 in 24 groups, 37 us with one key / value
+// head, whose 512 workgroups have 2048 waves to be given their runs.
 template <bool kFits>
 __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, BlockWin w, int32_t ratio,
                                                             uint32_t* d_flags) {
@@ -125,7 +127,8 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
   __shared__ uint32_t unsorted[kFits ? kSmall : 1];
   __shared__ int32_t near_table[kFits ? 2 * kSmall : 1], near_least[kFits ? 2 * kSmall : 1];
   __shared__ int32_t near_slot[kFits ? kSmall : 1], near_members[kFits ? kSmall : 1], near_base[kFits ? kSmall : 1];
-  __shared__ int64_t near_begin[2][kNear], near_run[2][kNear];
+  __shared__ int64_t near_begin[2][kNear];
+  __shared__ int64_t near_run[kMaxGroups * (1 + kWideWaves)];  // first unit of each run, the wide ones' in front
   __shared__ int32_t wide_number[kThreads], wide_units[kThreads];
   __shared__ int64_t sums[kWaves];
   __shared__ int32_t n_todo;
@@ -350,7 +353,7 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
   int64_t units[2], wide_cost = 0;  // (units: with those that stand for a tile's start)
   const int32_t start[2] = {kTileUnits, 0};
   int64_t* begin[2];
-  int64_t* run_at[2];
+  auto run_at = [&](int kind) { return near_run + kind * kMaxGroups; };
   for (int kind = 0; kind < 2; ++kind) {
     begin[kind] = n_tiles[kind] <= kNear ? near_begin[kind] : p.begin[kind];
     int64_t mine = 0;
@@ -379,7 +382,6 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
     runs[0] = (int32_t)min(n_wide, units[0]);
     runs[1] = (int32_t)min((p.groups - n_wide) * p.waves, units[1]);
   }
-  for (int kind = 0; kind < 2; ++kind) run_at[kind] = runs[kind] <= kNear ? near_run[kind] : p.run_at[kind];
   __syncthreads();
   // Rounds of whole tiles, as many as leave no workgroup (a thread each) above
   // the average; then `share` units more for each, the most evenly.
@@ -411,15 +413,15 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
     const int64_t skip = done < n_tiles[0] ? begin[0][done] : units[0];
     const int64_t at = block_scan(share, &total, sums);
     runs[0] = n_wide;
-    if (mine) run_at[0][tid] = skip + at;
+    if (mine) run_at(0)[tid] = skip + at;
   } else {
     for (int32_t r = tid; r < runs[0]; r += kThreads) {
-      run_at[0][r] = units[0] * r / runs[0];
+      run_at(0)[r] = units[0] * r / runs[0];
     }
   }
   // (counting a tile as a unit more made a batch of short contexts no faster, and one of
   // long ones slower: 241 -> 246 us)
-  for (int32_t r = tid; r < runs[1]; r += kThreads) run_at[1][r] = units[1] * r / runs[1];
+  for (int32_t r = tid; r < runs[1]; r += kThreads) run_at(1)[r] = units[1] * r / runs[1];
   __syncthreads();
   // What a wide run has without the tiles' starts; those that have something are numbered.
   auto before = [&](int64_t u) {
@@ -430,7 +432,7 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
   if (runs[0] > 0) {
     int32_t have = 0;
     if (tid < runs[0])
-      have = (int32_t)(before(tid + 1 < runs[0] ? run_at[0][tid + 1] : units[0]) - before(run_at[0][tid]));
+      have = (int32_t)(before(tid + 1 < runs[0] ? run_at(0)[tid + 1] : units[0]) - before(run_at(0)[tid]));
     int64_t total;
     const int64_t number = block_scan(have > 0, &total, sums);
     wide_units[tid] = have;
@@ -442,7 +444,7 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
     const int32_t whole = kind == 0 ? rounds * wide_groups : 0;
     // (a run that begins at the same unit as the next one is empty and not found)
     auto number_at = [&](int64_t u) {
-      const int32_t r = last_at_most(run_at[kind], runs[kind], u);
+      const int32_t r = last_at_most(run_at(kind), runs[kind], u);
       return kind == 0 ? wide_number[r] : r;
     };
     for (int32_t k = tid; k < n_tiles[kind]; k += kThreads) {
@@ -487,15 +489,21 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
       run.rounds = kind == 0 ? rounds : 0;
       run.stride = wide_groups;
       run.number = kind == 0 ? wide_number[r] : r;
-      const int64_t at = run_at[kind][r];
-      run.units = kind == 0 ? wide_units[r] : (int32_t)((r + 1 < runs[1] ? run_at[1][r + 1] : units[1]) - at);
+      const int64_t at = run_at(kind)[r];
+      run.units = kind == 0 ? wide_units[r] : (int32_t)((r + 1 < runs[1] ? run_at(1)[r + 1] : units[1]) - at);
       if (run.units > 0) {
         run.next = last_at_most(begin[kind], n_tiles[kind], at);
         run.from = max(0, (int32_t)(at - begin[kind][run.next]) - start[kind]);
       }
       if (run.rounds > 0 || run.units > 0) run.tile = p.tiles[kind][run.rounds > 0 ? r : run.next];
     }
-    p.runs[x] = run;
+    // (of an empty one only what says so)
+    if (run.rounds > 0 || run.units > 0) {
+      p.runs[x] = run;
+    } else {
+      p.runs[x].rounds = p.runs[x].units = 0;
+      p.runs[x].waves = run.waves;
+    }
   }
 
   // What is to be joined: the rows of own tiles that are kept, with their prefix

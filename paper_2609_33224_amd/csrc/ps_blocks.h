@@ -194,7 +194,6 @@ struct AttendPlanDev {
   AttendTile* tiles[2];
   int64_t* begin[2];  // first unit of each tile
   AttendRun* runs;     // of wave w of workgroup g: waves g + w
-  int64_t* run_at[2];  // first unit of each run, wide and narrow
   AttendJoin* joins;
   float* part;        // partial results: [head][slot rows][dim], weights as numerators
   float2* part_ml;    // their maxima (times scale * log2 e) and sums

@@ -135,7 +135,6 @@ hipError_t each_buffer(ps_attend_plan* p, F f) {
   for (int k = 0; k < 2; ++k) {
     one(d.tiles[k], d.tile_cap[k]);
     one(d.begin[k], d.tile_cap[k]);
-    one(d.run_at[k], (size_t)d.groups * (k == 0 ? 1 : kWideWaves));
   }
   // (a row with partial results each, or a place of empty rows: twice where two tiles have some)
   one(d.runs, d.n_runs);
