@@ -572,11 +572,11 @@ __device__ inline float top_of(const f32x16 (&s)[kB], float c) {
   return max_of_halves(top) * c;
 }
 
-// The running maximum (m, of scores times c) of the rows that say so becomes top; the sum and the results
-// follow it.  It need not be the row's own: rows say so where that is 2^8 above it or more. Weights of
-// some hundreds fit both types and are rounded to as many bits, and of 32 rows in random
-// order one has a new maximum in most steps, none so large a one.  (Whether a row says so depends on
-// the row alone, so its bits do not depend on what lies beside it.)
+// The running maximum (m, of scores times c) of the rows that say so becomes top; the sum and
+// the results follow it.  It need not be the row's own: rows say so where that is 2^8 above it
+// or more.  Weights of up to 2^13 fit both types and are rounded to as many bits, and of 32
+// rows in random order one has a new maximum in most steps, none so large a one.  (Whether a
+// row says so depends on the row alone, so its bits do not depend on what lies beside it.)
 template <int kDB>
 __device__ inline void raise_top(bool up, float top, float& m, float& l, f32x16 (&acc)[kDB]) {
   const float f = up ? __builtin_amdgcn_exp2f(m - top) : 1.0f;
