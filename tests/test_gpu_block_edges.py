@@ -1,0 +1,104 @@
+"""Attention over the block cache where its numbers are hard: large scores over long contexts, one
+weight that takes nearly all, infinite keys, extreme scales; needs an MI355X."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from tests.block_util import HALF, Window, values
+
+pytestmark = pytest.mark.gpu
+
+BF16, F16, E4M3 = torch.bfloat16, torch.float16, torch.float8_e4m3fn
+
+
+@pytest.fixture(scope="module")
+def ps():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2609_33224_amd as ps
+    return ps
+
+
+@pytest.fixture(scope="module")
+def sc(ps):
+    s = ps.Scorer(0)
+    yield s
+    s.close()
+
+
+def _gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def _randn(gen, *shape):
+    return torch.randn(shape, generator=gen, device="cuda")
+
+
+def _put(cache, name, w, r, x):
+    """Tokens 0 .. of request r's chain: x (token, KV head, element), e4m3 codes under the exponent 0."""
+    t = torch.arange(x.shape[0], device="cuda")
+    ch = torch.from_numpy(w.chain(r).astype(np.int64)).cuda()
+    buf = cache.tensors["kv".index(name)]
+    if buf.dtype == E4M3:
+        cache.tensors[2 + "kv".index(name)][ch[t // w.bt], :, t % w.bt] = 127
+        buf.view(torch.uint8)[ch[t // w.bt], :, t % w.bt] = x.to(E4M3).view(torch.uint8)
+    else:
+        buf[ch[t // w.bt], :, t % w.bt] = x.to(buf.dtype)
+
+
+def _run(sc, w, cache, q, scale=None, heads=None):
+    heads, dim = q.shape[1], q.shape[2]
+    out, lse = torch.full_like(q, 3.0), torch.full((w.n_rows, heads), 3.0, device="cuda")
+    p = sc.attend_plan(heads, cache.shape[0], dim, w.bt, w.n_req, w.n_rows)
+    p.build_dev(w.dev())
+    p.attend_dev(cache, q, out, lse, scale=scale)
+    torch.cuda.synchronize()
+    return out, lse
+
+
+def _token_values(cache, w, r, n):
+    """(k, v) of the first n tokens of request r's chain, in 64 bits: (token, KV head, element)."""
+    t, ch = np.arange(n), w.chain(r)
+    return [x[ch[t // w.bt], :, t % w.bt] for x in values(cache.tensors)]
+
+
+@pytest.mark.parametrize("dtype,typ", [(BF16, BF16), (F16, F16), (E4M3, BF16)])
+def test_a_long_share_keeps_its_sums(ps, sc, dtype, typ):
+    """Hundreds of steps by one wave, under a maximum of 100 to 200 that hardly moves: 256 requests of
+    32,768 tokens (the same pages, no prefix shared) for the 256 waves that each of 8 heads has.
+
+    Bounds as in check_attention: an exponent is off by dim 2^-24 of the sum of |q k| scale and 2^-20,
+    sums by (T / 16 + 16) 2^-24, the weights and the result by half a step of the type."""
+    heads, dim, bt, ctx, n = 8, 16, 64, 32768, 256
+    w = Window([0], [(0, ctx, 1)], bt)
+    w.reqs, w.ctx = np.repeat(w.reqs, n), np.repeat(w.ctx, n)
+    w.row_off, w.n_req, w.n_rows = np.arange(n + 1, dtype=np.int32), n, n
+    g = _gen(1)
+    c = ps.KvCache.empty(w.n_pages, heads, bt, dim, dtype)
+    k = 0.05 * _randn(g, ctx, heads, dim)
+    k[:, :, 0] = 25.0
+    _put(c, "k", w, 0, k)
+    _put(c, "v", w, 0, _randn(g, ctx, heads, dim) + torch.linspace(0, 8, ctx, device="cuda")[:, None, None])
+    q = _randn(g, n, heads, dim)
+    q[:, :, 0] = 16.0 + 16.0 * torch.rand(n, heads, generator=g, device="cuda")
+    q = q.to(typ)
+    out, lse = _run(sc, w, c, q)
+    kk, vv = (torch.from_numpy(x) for x in _token_values(c, w, 0, ctx))
+    h = HALF[typ]
+    for i in range(heads):
+        qi, scale = q[:, i].double().cpu(), dim ** -0.5
+        s = qi @ kk[:, i].T.contiguous() * scale
+        big = (qi.abs() @ kk[:, i].abs().T.contiguous()).amax(1) * scale
+        want = torch.logsumexp(s, 1)
+        p = torch.exp(s - want[:, None])
+        o, mag = p @ vv[:, i].contiguous(), p @ vv[:, i].abs().contiguous()
+        err = dim * 2.0 ** -24 * big + 2.0 ** -20 + (ctx / 16 + 16) * 2.0 ** -24
+        off = (lse[:, i].double().cpu() - want).abs()
+        assert (off <= err + 2.0 ** -22 * want.abs() + 2.0 ** -22).all(), (off / err).max()
+        off = (out[:, i].double().cpu() - o).abs()
+        # (fp16: weights below 2^-14 of the largest are none here, exp(-4) at the least)
+        assert (off <= h * o.abs() + (h + 2 * err[:, None]) * (1 + h) * mag).all()
+
+
