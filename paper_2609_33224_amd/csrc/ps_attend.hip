@@ -264,7 +264,12 @@ constexpr int key_stride(int DP) { return DP * 2 + 16; }
 // Positions of a narrow step: enough that a wave has 16 KB of a head of 128 in flight.
 constexpr int narrow_positions(bool kQ8, int DP) { return kQ8 && DP <= 128 ? 64 : 32; }
 
-template <bool kF16, bool kQ8, int DP, int RB>
+// A head of fewer than DP elements is padded (kPad): to those of q come zeros, and to those of its
+// keys too, since an infinity of a key times 0 would be NaN.  (A kernel of its own: with the
+// selects in it, chunks of full heads took 2.5% longer.)  The least such head:
+constexpr int least_dim(int DP) { return DP == 64 ? 16 : DP / 2 + 16; }
+
+template <bool kF16, bool kQ8, int DP, bool kPad, int RB>
 __device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char* vs) {
   constexpr int kTok = narrow_positions(kQ8, DP);
   constexpr int kH = kTok / 16;                       // rows of positions in the first product
@@ -300,8 +305,8 @@ __device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char*
       const Spot s = spot_of(a, p.head, page[h], min(t + 16 * h + col, last));
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
-        // (where the head has fewer elements than DP, its last ones once more: they
-        // meet zeros of q, and results that nobody reads)
+        // (where the head has fewer elements than DP, its last ones once more: of keys they
+        // become zeros before they are used, of values they make results that nobody reads)
         const int d = kQ8 ? min(64 * i + 16 * g, D - 16) : min(32 * i + 8 * g, D - 8);
         const int64_t at = kQ8 ? s.at + d : 2 * (s.at + d);
         kr[h][i] = *(const u32x4*)(a.cache.k + at);
@@ -365,6 +370,13 @@ __device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char*
           *(u32x4*)(vs + row * kV + (4 * i + g) * 16) = vr[h][i];
         }
       }
+    if constexpr (kPad) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+        if ((kQ8 ? 64 : 32) * (i + 1) > least_dim(DP) && (kQ8 ? 64 * i + 16 * g : 32 * i + 8 * g) >= D)
+#pragma unroll
+          for (int h = 0; h < kH; ++h) kr[h][i] = u32x4{0, 0, 0, 0};
+    }
     // scores: position 16 h + 4 g + i of the step, row b * 16 + col
     f32x4 s[RB][kH];
 #pragma unroll
@@ -484,11 +496,12 @@ constexpr int wide_positions(int DP) { return DP <= 128 ? 64 : 32; }
 
 // What a thread of a wide or tall tile's workgroup stages: part of one row of a step's
 // positions, asked for (pages, then loads) before it is put into shared memory.
-template <bool kF16, bool kQ8, int DP, int kTok, int kThreads>
+template <bool kF16, bool kQ8, int DP, bool kPad, int kTok, int kThreads>
 struct Stage {
   static constexpr int kPer = kThreads / kTok;                     // threads that stage a row
   static constexpr int kLoads = (kQ8 ? DP / 16 : DP / 8) / kPer;  // 16-byte loads per thread
   static constexpr int kChunk = kQ8 ? 32 : 16;                     // bytes in shared memory of such a load
+  static constexpr int kEach = kQ8 ? 16 : 8;                       // elements
   const int row, sc;  // thread x: row x / kPer, chunks x % kPer + kPer i
   const int32_t last;
   uint32_t page, slot;
@@ -519,8 +532,13 @@ struct Stage {
   }
   // Into the step's keys and values; whether values had infinities or NaN, which are
   // taken out of a masked step's (as in the narrow kernel).
-  __device__ uint32_t put(unsigned char* keys, unsigned char* values, bool masked) {
+  __device__ uint32_t put(unsigned char* keys, unsigned char* values, bool masked, int D) {
     uint32_t odd = 0;
+    if constexpr (kPad) {  // (as in the narrow kernel)
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+        if (kEach * kPer * (i + 1) > least_dim(DP) && kEach * (kPer * i + sc) >= D) kr[i] = u32x4{0, 0, 0, 0};
+    }
     unsigned char* ks = keys + row * key_stride(DP) + sc * kChunk;
     unsigned char* vs = values + row * value_stride(DP) + sc * kChunk;
 #pragma unroll
@@ -643,7 +661,7 @@ __device__ inline u32x4 turned_values(const unsigned char* at, int stride) {
 // kSplit = 1: each wave has 32 of the 128 rows and all positions of a step; 2: 32 of 64
 // rows and half of the positions, the halves' results joined at the end, so that
 // tiles of 64 rows keep all four SIMDs at work.
-template <bool kF16, bool kQ8, int DP, int kSplit>
+template <bool kF16, bool kQ8, int DP, bool kPad, int kSplit>
 __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* smem, int32_t* odd_at) {
   constexpr int kSteps = DP / 16;
   constexpr int kTok = wide_positions(DP);
@@ -664,12 +682,12 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
     for (int i = 0; i < 16; ++i) acc[k][i] = 0;
   float m = -INFINITY, l = 0;  // (the maximum of scores times c)
 
-  Stage<kF16, kQ8, DP, kTok, 256> st(p, wave, lane);
+  Stage<kF16, kQ8, DP, kPad, kTok, 256> st(p, wave, lane);
   // (of one request's rows the first sees least; those of a shared prefix see all of it)
   const int32_t least_of_all = min(uniform(a.plan.lim[row_at(a, p, 0).place]), p.tb);
   auto stage = [&](int buf, int32_t t) {
     unsigned char* keys = smem + buf * kTile;
-    if (st.put(keys, keys + kKeys, t + kTok > least_of_all))
+    if (st.put(keys, keys + kKeys, t + kTok > least_of_all, a.cache.dim))
       odd_at[buf] = t;  // (a value left by another piece only costs a look)
   };
 
@@ -802,7 +820,7 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
 // wide kernel's tiles, 1060 to 1090 with these, of 1180 that a large matrix product reaches.
 constexpr int kTallStep = 64;
 
-template <bool kF16, bool kQ8, int DP>
+template <bool kF16, bool kQ8, int DP, bool kPad>
 __device__ void tall_piece(const AttendArgs& a, const Piece& p, unsigned char* smem, int32_t* odd_at) {
   constexpr int kSteps = DP / 16, kTok = kTallStep, kDB = DP / 32;
   constexpr int kK = key_stride(DP), kV = value_stride(DP);
@@ -822,10 +840,10 @@ __device__ void tall_piece(const AttendArgs& a, const Piece& p, unsigned char* s
     for (int i = 0; i < 16; ++i) acc[k][i] = 0;
   float m = -INFINITY, l = 0;  // (the maximum of scores times c)
 
-  Stage<kF16, kQ8, DP, kTok, 512> st(p, wave, lane);
+  Stage<kF16, kQ8, DP, kPad, kTok, 512> st(p, wave, lane);
   const int32_t least_of_all = min(uniform(a.plan.lim[row_at(a, p, 0).place]), p.tb);  // (as in the wide kernel)
   auto stage = [&](int kb, int vb, int32_t t) {
-    if (st.put(smem + kb * kKeys, smem + 2 * kKeys + vb * kValues, t + kTok > least_of_all))
+    if (st.put(smem + kb * kKeys, smem + 2 * kKeys + vb * kValues, t + kTok > least_of_all, a.cache.dim))
       odd_at[vb] = t;
   };
   st.pages(a, p, p.ta);
@@ -951,7 +969,7 @@ constexpr int shared_bytes(bool kQ8, int DP, bool kTall) {
   return wide > narrow ? wide : narrow;
 }
 
-template <bool kF16, bool kQ8, int DP, bool kTall>
+template <bool kF16, bool kQ8, int DP, bool kTall, bool kPad>
 __global__ __launch_bounds__(64 * (kTall ? kTallWaves : kWideWaves), DP <= 128 ? 2 : 1) void attend_kernel(AttendArgs a) {
   constexpr int kWaves = kTall ? kTallWaves : kWideWaves;
   __shared__ __align__(16) unsigned char smem[shared_bytes(kQ8, DP, kTall)];
@@ -1002,13 +1020,13 @@ __global__ __launch_bounds__(64 * (kTall ? kTallWaves : kWideWaves), DP <= 128 ?
     p.tb = min(t1, t0 + (from + n) * kUnit);
     p.slot = slot < 0 ? -1 : slot + (piece - uniform(t.first)) * p.rows;
     if constexpr (kTall) {
-      if (kind == 0) tall_piece<kF16, kQ8, DP>(a, p, smem, odd_at);
+      if (kind == 0) tall_piece<kF16, kQ8, DP, kPad>(a, p, smem, odd_at);
     } else {
-      if (kind == 0 && DP <= 128 && p.rows <= 64) wide_piece<kF16, kQ8, DP, DP <= 128 ? 2 : 1>(a, p, smem, odd_at);
-      else if (kind == 0) wide_piece<kF16, kQ8, DP, 1>(a, p, smem, odd_at);
+      if (kind == 0 && DP <= 128 && p.rows <= 64) wide_piece<kF16, kQ8, DP, kPad, DP <= 128 ? 2 : 1>(a, p, smem, odd_at);
+      else if (kind == 0) wide_piece<kF16, kQ8, DP, kPad, 1>(a, p, smem, odd_at);
     }
     if (kind == 1)
-      narrow_piece<kF16, kQ8, DP, kNarrowRows / 16>(a, p, smem + wave * narrow_positions(kQ8, DP) * narrow_stride(DP));
+      narrow_piece<kF16, kQ8, DP, kPad, kNarrowRows / 16>(a, p, smem + wave * narrow_positions(kQ8, DP) * narrow_stride(DP));
     if (most != INT32_MAX) left -= n;
   }
 }
@@ -1119,19 +1137,25 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
   }
 }
 
-template <bool kF16, bool kQ8, int DP>
+template <bool kF16, bool kQ8, int DP, bool kPad>
 void launch(const AttendArgs& a, int32_t num_cus, hipStream_t s) {
   const dim3 grid((unsigned)(a.plan.groups * a.cache.heads));
   const dim3 join((unsigned)std::min<int64_t>((int64_t)a.win.n_rows * a.heads, 8 * num_cus));
   if constexpr (DP == 128) {
     if (a.plan.waves == kTallWaves) {
-      hipLaunchKernelGGL((attend_kernel<kF16, kQ8, DP, true>), grid, dim3(64 * kTallWaves), 0, s, a);
+      hipLaunchKernelGGL((attend_kernel<kF16, kQ8, DP, true, kPad>), grid, dim3(64 * kTallWaves), 0, s, a);
       hipLaunchKernelGGL((join_kernel<kF16, DP / 4>), join, dim3(256), 0, s, a);
       return;
     }
   }
-  hipLaunchKernelGGL((attend_kernel<kF16, kQ8, DP, false>), grid, dim3(64 * kWideWaves), 0, s, a);
+  hipLaunchKernelGGL((attend_kernel<kF16, kQ8, DP, false, kPad>), grid, dim3(64 * kWideWaves), 0, s, a);
   hipLaunchKernelGGL((join_kernel<kF16, DP / 4>), join, dim3(256), 0, s, a);
+}
+
+template <bool kF16, bool kQ8, int DP>
+void launch_dim(const AttendArgs& a, int32_t num_cus, hipStream_t s) {
+  if (a.cache.dim < DP) launch<kF16, kQ8, DP, true>(a, num_cus, s);
+  else launch<kF16, kQ8, DP, false>(a, num_cus, s);
 }
 
 }  // namespace
@@ -1154,9 +1178,9 @@ hipError_t ps_launch_attend(const ps::AttendArgs& a, int32_t num_cus, hipStream_
   const bool f16 = a.q.dtype == PS_T_F16, quant = a.cache.dtype == PS_T_E4M3;
 #define PS_DIM(F, Q)                                                       \
   do {                                                                     \
-    if (a.cache.dim <= 64) ps::launch<F, Q, 64>(a, num_cus, s);            \
-    else if (a.cache.dim <= 128) ps::launch<F, Q, 128>(a, num_cus, s);     \
-    else ps::launch<F, Q, 256>(a, num_cus, s);                             \
+    if (a.cache.dim <= 64) ps::launch_dim<F, Q, 64>(a, num_cus, s);        \
+    else if (a.cache.dim <= 128) ps::launch_dim<F, Q, 128>(a, num_cus, s); \
+    else ps::launch_dim<F, Q, 256>(a, num_cus, s);                         \
   } while (0)
   if (f16 && quant) PS_DIM(true, true);
   else if (f16) PS_DIM(true, false);

@@ -102,3 +102,40 @@ def test_a_long_share_keeps_its_sums(ps, sc, dtype, typ):
         assert (off <= h * o.abs() + (h + 2 * err[:, None]) * (1 + h) * mag).all()
 
 
+# rows of a request by the head: the kernels' tiles of 16, 64 (positions split), 128 and 256 rows
+TILES = [("narrow", 4, 1), ("split", 40, 1), ("wide", 128, 1), ("tall", 64, 64)]
+
+
+@pytest.mark.parametrize("tile,heads,n", TILES)
+@pytest.mark.parametrize("dim", [16, 48, 64, 80, 96, 112, 128, 144, 208, 256])
+@pytest.mark.parametrize("dtype,typ", [(BF16, BF16), (F16, F16), (E4M3, F16)])
+def test_keys_of_minus_infinity_have_no_weight(ps, sc, tile, heads, n, dim, dtype, typ):
+    """Keys whose score is -inf, by an infinity among the last elements of the head, give the bits that keys
+    of a very low score give (exp2 of both is 0), at every head size.  e4m3: an infinity in fp16, to which
+    the value is converted."""
+    bt, ctx = 16, 200
+    w = Window([0], [(0, ctx, n)], bt, seed=dim)
+    g = _gen(dim)
+    c = ps.KvCache.empty(w.n_pages, 1, bt, dim, dtype)
+    _put(c, "k", w, 0, _randn(g, ctx, 1, dim))
+    _put(c, "v", w, 0, _randn(g, ctx, 1, dim))
+    q = _randn(g, n, heads, dim)
+    q[..., dim - 3], q[..., dim - 5] = 2.0, -2.0
+    q = q.to(typ)
+    ch = w.chain(0)
+    got = []
+    for low in (-30000.0, -math.inf):
+        for t, e, sign in ((0, dim - 3, 1), (21, dim - 5, -1), (130, dim - 3, 1), (ctx - 2, dim - 5, -1)):
+            at = int(ch[t // bt]), 0, t % bt
+            if dtype == E4M3:  # 448 * 2^6 and 448 * 2^10
+                c.tensors[0][at].view(torch.uint8).zero_()
+                c.tensors[0][at][e:e + 1] = torch.tensor([-448.0 * sign], device="cuda").to(E4M3)
+                c.tensors[2][at] = 127 + (6 if math.isfinite(low) else 10)
+            else:
+                c.tensors[0][at][e] = low * sign
+        got.append(_run(sc, w, c, q))
+    (a, la), (b, lb) = got
+    assert torch.isfinite(a).all() and torch.isfinite(la).all()
+    assert torch.equal(a, b) and torch.equal(la, lb)
+
+
