@@ -578,8 +578,9 @@ ps_status ps_attend_plan_dev(ps_attend_plan* plan, const ps_kv_window* window, u
  * natural logarithm of the sum of exp(scale * q . k_t).  Products take the
  * operands in q's 16-bit type (PS_T_E4M3 values are converted to it; a 16-bit
  * cache is of q's type), sums and the softmax are in fp32, the softmax's
- * weights are rounded to that type before they multiply v.  A row without a
- * token gives zeros and -inf.  What lies in the pages behind a row's position
+ * weights are rounded to that type before they multiply v (fp16: a weight of
+ * less than 2^-24 of the row's largest loses bits, and is off by 2^-35 of it
+ * at most).  A row without a token gives zeros and -inf.  What lies in the pages behind a row's position
  * does not reach it, whatever its bits.  Results do not depend on the run: the
  * same window gives the same bits.  out must not overlap q or the cache.
  * Asynchronous on `hip_stream`, no allocation.  The plan's memory is in use

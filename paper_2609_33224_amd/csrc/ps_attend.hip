@@ -25,7 +25,10 @@
 // Scores, maxima, sums and results are in fp32 throughout.  Two things are rounded to the
 // 16-bit type: the weights, which the second product takes in it (each by half a step at
 // most, 2^-8 of its own size in bf16 and 2^-11 in fp16, so a result by no more than that of
-// sum p |v|; the sum that divides them takes them as they were), and the result.
+// sum p |v|; the sum that divides them takes them as they were), and the result.  fp16 has
+// no such half step below 2^-14, where a weight is off by 2^-25: there all weights are 2^10
+// times what they stand for (weight_lift), a row's largest is 2^10 at least, and T small
+// ones are off by T 2^-35 max|v| in the result at most.
 
 #include <algorithm>
 
@@ -46,6 +49,26 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLn2 = 0.693147180559945309f;
+
+// The exponent that weights are lifted by, so that fp16 keeps the bits of small ones (a token that
+// takes nearly all of the weight, with a small value, leaves the result to them: 4096 weights of
+// 1.5 * 2^-24 made it a third too large).  The running maximum that is kept is less by it.
+// Weights reach 2^10 where it is the row's, up to 2^raise_by more where it lies below, of fp16's
+// 2^16: the rest is for the rounding of score x c, which shifts all weights of a row alike (by less
+// than 2^2 for scores below 2^26).  bf16 has fp32's range.
+constexpr float weight_lift(bool kF16) { return kF16 ? 10.0f : 0.0f; }
+// How far a wide tile's row may outgrow the running maximum before that follows.
+constexpr float raise_by(bool kF16) { return kF16 ? 4.0f : 8.0f; }
+// A tall tile looks for the maximum where a lane's 32 weights sum up to more: above 32 times the lifted
+// largest weight, and no weight that leaves fp16.
+constexpr float far_sum(bool kF16) { return kF16 ? 49152.0f : 8192.0f; }
+
+// The logarithm of a sum l of lifted weights under the kept maximum m.
+template <bool kF16>
+__device__ inline float lse_of(float m, float l) {
+  const float lift = weight_lift(kF16);
+  return __builtin_fmaf(m + lift, kLn2, __logf(l * __builtin_exp2f(-lift)));
+}
 
 template <bool kF16>
 __device__ inline f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
@@ -236,8 +259,9 @@ __device__ inline void put4(const AttendArgs& a, const Piece& p, int32_t r, int3
   *(u32x2*)(a.out.data + 2 * ((int64_t)a.plan.row[w.place] * a.out.row + (int64_t)w.head * a.out.head + d)) = x;
 }
 
-// A row's maximum (mc: of scores times c) and sum, likewise; returns what its results are
+// A row's maximum (mc: of scores times c, less weight_lift) and sum, likewise; returns what its results are
 // multiplied by where they are final.
+template <bool kF16>
 __device__ inline float put_ml(const AttendArgs& a, const Piece& p, int32_t r, float mc, float l, bool write) {
   if (p.slot >= 0) {
     if (write) a.plan.part_ml[(int64_t)p.head * a.plan.slot_rows + p.slot + r] = float2{mc, l};
@@ -247,7 +271,7 @@ __device__ inline float put_ml(const AttendArgs& a, const Piece& p, int32_t r, f
   const bool empty = a.plan.lim[w.place] <= 0;
   if (write && a.lse)
     a.lse[(int64_t)a.plan.row[w.place] * a.heads + w.head] =
-        empty ? -INFINITY : __builtin_fmaf(mc, kLn2, __logf(l));
+        empty ? -INFINITY : lse_of<kF16>(mc, l);
   return empty ? 0.0f : 1.0f / l;
 }
 
@@ -282,7 +306,7 @@ __device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char*
   const int D = a.cache.dim;
 
   f32x4 acc[RB][kDB];
-  float m[RB], l[RB];  // (the maximum of scores times c)
+  float m[RB], l[RB];  // (the maximum of scores times c, less weight_lift)
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
     m[b] = -INFINITY;
@@ -423,7 +447,7 @@ __device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char*
       // (kept as the rounded product that the weights take, so that the factor of a maximum that has
       // not moved is 1: a fused m c - mc is the product's rounding error, the same in every step, and
       // bent the sums of 1024 steps under scores of 100 to 200 by 4e-3)
-      const float nm = fmaxf(m[b], top * p.c);
+      const float nm = fmaxf(m[b], top * p.c - weight_lift(kF16));
       mc[b] = nm == -INFINITY ? 0.0f : nm;
       const float f = __builtin_amdgcn_exp2f(m[b] - mc[b]);
       m[b] = nm;
@@ -482,7 +506,7 @@ __device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char*
     l[b] += __shfl_xor(l[b], 32, 64);
     const int32_t r = b * 16 + (at & 15);
     if (r < p.rows) {
-      const float inv = put_ml(a, p, r, m[b], l[b], d0 == 0);
+      const float inv = put_ml<kF16>(a, p, r, m[b], l[b], d0 == 0);
 #pragma unroll
       for (int k = 0; k < kDB; ++k) put4<kF16>(a, p, r, 16 * k + d0, acc[b][k], inv);
     }
@@ -584,18 +608,18 @@ __device__ inline void mask_scores(f32x16 (&s)[kB], int32_t t, int hb, int32_t e
       if (t + 32 * b + 8 * (i >> 2) + 4 * hb + (i & 3) >= end) s[b][i] = -INFINITY;
 }
 
-// The largest of a row's scores, times c.
-template <int kB>
+// The largest of a row's scores, times c, less weight_lift.
+template <bool kF16, int kB>
 __device__ inline float top_of(const f32x16 (&s)[kB], float c) {
   float top = s[0][0];
 #pragma unroll
   for (int i = 1; i < 16 * kB; ++i) top = fmaxf(top, s[i >> 4][i & 15]);
-  return max_of_halves(top) * c;
+  return max_of_halves(top) * c - weight_lift(kF16);
 }
 
 // The running maximum (m, of scores times c) of the rows that say so becomes top; the sum and
 // the results follow it.  It need not be the row's own: rows say so where that is 2^8 above it
-// or more.  Weights of up to 2^13 fit both types and are rounded to as many bits, and of 32
+// (fp16: 2^4) or more.  Such weights fit both types and are rounded to as many bits, and of 32
 // rows in random order one has a new maximum in most steps, none so large a one.  (Whether a
 // row says so depends on the row alone, so its bits do not depend on what lies beside it.)
 template <int kDB>
@@ -643,7 +667,7 @@ __device__ inline void put_rows(const AttendArgs& a, const Piece& p, int rows0, 
   const int at = fresh(lane), d0 = 4 * (at >> 5);
   const int32_t r = rows0 + (at & 31);
   if (r >= p.rows) return;
-  const float inv = put_ml(a, p, r, m, l, d0 == 0);
+  const float inv = put_ml<kF16>(a, p, r, m, l, d0 == 0);
 #pragma unroll
   for (int k = 0; k < kDB; ++k)
 #pragma unroll
@@ -680,7 +704,7 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
   for (int k = 0; k < kDB; ++k)
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[k][i] = 0;
-  float m = -INFINITY, l = 0;  // (the maximum of scores times c)
+  float m = -INFINITY, l = 0;  // (the maximum of scores times c, less weight_lift)
 
   Stage<kF16, kQ8, DP, kPad, kTok, 256> st(p, wave, lane);
   // (of one request's rows the first sees least; those of a shared prefix see all of it)
@@ -733,8 +757,8 @@ __device__ void wide_piece(const AttendArgs& a, const Piece& p, unsigned char* s
       }
       const bool masked = t + kTok > p.tb || t + kTok > least;
       if (masked) mask_scores(s, t + off0, hb, min(lim, p.tb));
-      const float top = top_of(s, p.c);
-      const bool up = top > m + 8.0f;
+      const float top = top_of<kF16>(s, p.c);
+      const bool up = top > m + raise_by(kF16);
       if (__any(up)) raise_top(up, top, m, l, acc);
       const float mc = m == -INFINITY ? 0.0f : m;
       // (also for a wave whose rows all see all of the step)
@@ -838,7 +862,7 @@ __device__ void tall_piece(const AttendArgs& a, const Piece& p, unsigned char* s
   for (int k = 0; k < kDB; ++k)
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[k][i] = 0;
-  float m = -INFINITY, l = 0;  // (the maximum of scores times c)
+  float m = -INFINITY, l = 0;  // (the maximum of scores times c, less weight_lift)
 
   Stage<kF16, kQ8, DP, kPad, kTok, 512> st(p, wave, lane);
   const int32_t least_of_all = min(uniform(a.plan.lim[row_at(a, p, 0).place]), p.tb);  // (as in the wide kernel)
@@ -905,13 +929,14 @@ __device__ void tall_piece(const AttendArgs& a, const Piece& p, unsigned char* s
     if (masked) mask_scores(s, t, hb, min(lim, p.tb));
     if (t + kTok > least_of_all && odd_at[vb] == t) {
       // (rows without a maximum take theirs first: their results are multiplied by 0 then)
-      const float top = top_of(s, p.c);
+      const float top = top_of<kF16>(s, p.c);
       raise_top(m == -INFINITY && top > m, top, m, l, acc);
       add_odd<kF16, kQ8>(a, p, t, min(t + kTok, p.tb), hb, lim, acc);
     }
     // Weights from the maximum as it is, which is nearly always near enough.  The row's own is
-    // looked for where there is none yet, or where a lane's 32 weights sum up to 2^13,
-    // so that one of them is 2^8 at least (and none leaves fp16).
+    // looked for where there is none yet, or where a lane's 32 weights sum up to 2^13 (fp16:
+    // 1.5 * 2^15), so that one of them is 2^8 (2^0.5 times the lifted 1) at least and none
+    // leaves the type.
     auto all_weights = [&] {
       const float mc = m == -INFINITY ? 0.0f : m;
       float sum = 0;
@@ -920,9 +945,9 @@ __device__ void tall_piece(const AttendArgs& a, const Piece& p, unsigned char* s
       return sum;
     };
     float sum = all_weights();
-    const uint64_t far = __ballot(sum > 8192.0f || m == -INFINITY);
+    const uint64_t far = __ballot(sum > far_sum(kF16) || m == -INFINITY);
     if (far) {
-      const float top = top_of(s, p.c);
+      const float top = top_of<kF16>(s, p.c);
       raise_top((far | far >> 32) >> col & 1 && top > m, top, m, l, acc);
       sum = all_weights();
     }
@@ -1133,7 +1158,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
       *(u32x2*)(a.out.data + 2 * (row * a.out.row + (int64_t)h * a.out.head + d)) = w;
     }
     if (writes && a.lse && lane == 0)
-      a.lse[row * a.heads + h] = x.empty ? -INFINITY : __builtin_fmaf(top, kLn2, __logf(l));
+      a.lse[row * a.heads + h] = x.empty ? -INFINITY : lse_of<kF16>(top, l);
   }
 }
 
