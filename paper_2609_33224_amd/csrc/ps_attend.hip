@@ -1009,11 +1009,11 @@ __global__ __launch_bounds__(64 * (kTall ? kTallWaves : kWideWaves), DP <= 128 ?
   p.c = fmaxf(fabsf(c), 1.17549435e-38f);  // (not 0: it multiplies infinities)
   p.neg = c < 0 ? 0x80008000u : 0u;
   // (scalars throughout: what is loaded after the first store would be a lane's otherwise)
+  const AttendHead plan = *a.plan.head;
   const AttendRun run = a.plan.runs[group * kWaves + wave];
   const int32_t kind = uniform(run.kind), rounds = uniform(run.rounds), number = uniform(run.number);
   int32_t next = uniform(run.next), at = uniform(run.from), left = uniform(run.units);
-  // (a plan for workgroups of another size: the window planned last was not this launch's)
-  if (uniform(run.waves) != kWaves) return;
+  if (!plan_is_for(plan, a.win, kWaves)) return;
   bool first = true;
   for (int32_t round = 0;;) {
     int32_t k, from, most, piece;
@@ -1071,7 +1071,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int32_t D = a.cache.dim;
   const AttendHead plan = *a.plan.head;
-  if (plan.waves != a.plan.waves) return;  // (as in the attention kernel)
+  if (!plan_is_for(plan, a.win, a.plan.waves)) return;
   const int64_t n = (int64_t)plan.n_joins * a.cache.heads;
   const bool together = n <= gridDim.x;  // (the same for the grid)
   const int64_t first = together ? blockIdx.x : (int64_t)blockIdx.x * 4 + wave;

@@ -155,7 +155,7 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
   if (__syncthreads_or(bad)) {
     if (d_flags)
       for (int32_t r = tid; r < n; r += kThreads) d_flags[r] = PS_R_INVALID;
-    if (tid == 0) *p.head = AttendHead{0, p.waves};
+    if (tid == 0) *p.head = AttendHead{w.pages, w.pages_len, w.n_rows, p.waves, 0, 0};
     for (int32_t x = tid; x < p.n_runs; x += kThreads) p.runs[x].rounds = p.runs[x].units = 0;
     return;
   }
@@ -484,7 +484,6 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
     const int32_t r = kind == 0 ? g : g - wide_groups + x % p.waves * (p.groups - wide_groups);
     AttendRun run{};
     run.kind = kind;
-    run.waves = p.waves;
     if (g < p.groups && r < runs[kind]) {
       run.rounds = kind == 0 ? rounds : 0;
       run.stride = wide_groups;
@@ -498,12 +497,8 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
       if (run.rounds > 0 || run.units > 0) run.tile = p.tiles[kind][run.rounds > 0 ? r : run.next];
     }
     // (of an empty one only what says so)
-    if (run.rounds > 0 || run.units > 0) {
-      p.runs[x] = run;
-    } else {
-      p.runs[x].rounds = p.runs[x].units = 0;
-      p.runs[x].waves = run.waves;
-    }
+    if (run.rounds > 0 || run.units > 0) p.runs[x] = run;
+    else p.runs[x].rounds = p.runs[x].units = 0;
   }
 
   // What is to be joined: the rows of own tiles that are kept, with their prefix
@@ -559,7 +554,7 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
         push(s.p0 + j, -1, nullptr, -1, 0);
   }
   __syncthreads();
-  if (tid == 0) *p.head = AttendHead{n_todo, p.waves};
+  if (tid == 0) *p.head = AttendHead{w.pages, w.pages_len, w.n_rows, p.waves, n_todo, 0};
 }
 
 }  // namespace

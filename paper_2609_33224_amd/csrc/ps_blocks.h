@@ -160,10 +160,20 @@ struct alignas(16) AttendJoin {
   int32_t pad[3];
 };
 
+// What the plan was made for.  An attention that was captured alone runs on whatever plan its memory
+// holds when it is replayed: one for other workgroups or another window's pages and rows, whose
+// offsets and rows may lie behind this one's buffers, is not run.
 struct AttendHead {
-  int32_t n_joins;
+  const int32_t* pages;
+  int64_t pages_len;
+  int32_t n_rows;
   int32_t waves;  // AttendPlanDev::waves when the plan was made
+  int32_t n_joins;
+  int32_t pad;
 };
+__device__ inline bool plan_is_for(const AttendHead& h, const BlockWin& w, int32_t waves) {
+  return h.pages == w.pages && h.pages_len == w.pages_len && h.n_rows == w.n_rows && h.waves == waves;
+}
 
 // What a wave of a workgroup takes: (wide tiles, all waves the same) `rounds` whole
 // tiles, one of each `stride` of them (tile_of_round), then `units` from unit `from` of tile `next` on.
@@ -172,10 +182,9 @@ struct alignas(16) AttendRun {
   AttendTile tile;
   int32_t number;  // of the runs of its kind that have units
   int32_t kind;    // 0: wide, 1: narrow
-  int32_t waves;   // AttendHead::waves
   int32_t rounds, stride;
   int32_t next, from, units;
-  int32_t pad[2];
+  int32_t pad[3];
 };
 
 struct AttendPlanDev {

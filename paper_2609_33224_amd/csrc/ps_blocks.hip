@@ -229,7 +229,10 @@ ps_status ps_attend_plan_create(ps_ctx* c, int32_t n_heads, int32_t n_kv_heads, 
   p->max_req = max_req;
   p->max_rows = max_rows;
   size_plan(p, c->num_cus);
-  const hipError_t e = each_buffer(p, [&](auto*& ptr, size_t bytes) { return c->pool.grow(&ptr, bytes); });
+  hipError_t e = each_buffer(p, [&](auto*& ptr, size_t bytes) { return c->pool.grow(&ptr, bytes); });
+  // (no window's plan: an attention that runs before the first one does nothing)
+  if (e == hipSuccess) e = hipMemsetAsync(p->dev.head, 0, sizeof(AttendHead), c->stream);
+  if (e == hipSuccess) e = hipStreamSynchronize(c->stream);
   if (e != hipSuccess) {
     release(p);
     delete p;

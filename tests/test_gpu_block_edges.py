@@ -183,3 +183,63 @@ def test_small_weights_of_half_precision(ps, sc, tile, heads, n, dim, dtype, bel
         assert (off <= err + 2.0 ** -22 * z.abs() + 2.0 ** -22).all()
 
 
+def test_attention_captured_alone_runs_on_its_own_windows_plan_only(ps, sc):
+    """Another window planned in between, of another pages buffer, a longer one or more rows: its pages and rows may
+    lie behind this one's buffers, so nothing is written.  The first one planned again: its results."""
+    heads, kv, dim, bt, n = 8, 2, 64, 16, 6
+    w = Window([2], [(0, 32 + 9 * k, 1) for k in range(n)], bt)
+    c = ps.KvCache.empty(400, kv, bt, dim)
+    q, out = _randn(_gen(1), n, heads, dim).bfloat16(), torch.zeros(n, heads, dim, dtype=BF16, device="cuda")
+    lse = torch.zeros(n, heads, device="cuda")
+    for name in "kv":
+        for r in range(n):
+            _put(c, name, w, r, _randn(_gen(r), int(w.ctx[r]), kv, dim))
+    win = w.dev()
+    others = [w.dev(),
+              Window([2], [(0, 32 + 9 * k, 1) for k in range(n)], bt, spare=9).dev(),
+              Window([20], [(0, 400 + 9 * k, 1) for k in range(n)], bt).dev(),
+              Window([2], [(0, 32 + 9 * k, 2) for k in range(n)], bt).dev()]
+    p = sc.attend_plan(heads, kv, dim, bt, n, 2 * n)
+    p.build_dev(win)
+    p.attend_dev(c, q, out, lse)
+    ref, lref = out.clone(), lse.clone()
+    assert torch.isfinite(lref).all()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        p.attend_dev(c, q, out, lse)
+    for other in others:
+        out.fill_(3.0)
+        lse.fill_(3.0)
+        p.build_dev(other)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert (out == 3).all() and (lse == 3).all()
+        p.build_dev(win)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, ref) and torch.equal(lse, lref)
+
+
+def test_a_plan_that_was_only_captured_is_no_plan_yet(ps, sc):
+    heads, kv, dim, bt = 8, 2, 64, 16
+    w = Window([2], [(0, 40, 1), (0, 50, 2)], bt)
+    win, c = w.dev(), ps.KvCache.empty(w.n_pages, kv, bt, dim)
+    q = _randn(_gen(1), w.n_rows, heads, dim).bfloat16()
+    for _ in range(2):  # (the second one where the first one's memory was)
+        p, out = sc.attend_plan(heads, kv, dim, bt, 2, 3), torch.full_like(q, 3.0)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            p.build_dev(win)
+            p.attend_dev(c, q, out)
+        p.attend_dev(c, q, out)
+        torch.cuda.synchronize()
+        assert (out == 3).all()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert (out == 0).all()
+        del graph
+        p.close()
+
+
