@@ -52,7 +52,7 @@ constexpr float kLn2 = 0.693147180559945309f;
 
 // The exponent that weights are lifted by, so that fp16 keeps the bits of small ones (a token that
 // takes nearly all of the weight, with a small value, leaves the result to them: 4096 weights of
-// 1.5 * 2^-24 made it a third too large).  The running maximum that is kept is less by it.
+// 2^-23.4 made it up to 17% too large).  The running maximum that is kept is less by it.
 // Weights reach 2^10 where it is the row's, up to 2^raise_by more where it lies below, of fp16's
 // 2^16: the rest is for the rounding of score x c, which shifts all weights of a row alike (by less
 // than 2^2 for scores below 2^26).  bf16 has fp32's range.

@@ -139,47 +139,53 @@ def test_keys_of_minus_infinity_have_no_weight(ps, sc, tile, heads, n, dim, dtyp
     assert torch.equal(a, b) and torch.equal(la, lb)
 
 
-@pytest.mark.parametrize("tile,heads,n", TILES)
+# the same, with as many requests as make a wave's or a workgroup's share a whole context
+LONG = [("narrow", 4, 1, 256), ("split", 40, 1, 64), ("wide", 128, 1, 64), ("tall", 64, 64, 4)]
+
+
+@pytest.mark.parametrize("tile,ratio,n,n_req", LONG)
 @pytest.mark.parametrize("dim", [64, 128, 256])
 @pytest.mark.parametrize("dtype", [F16, E4M3])
 @pytest.mark.parametrize("below", [17.6, 20.6, 23.4])
 @pytest.mark.parametrize("alike", [True, False])
-def test_small_weights_of_half_precision(ps, sc, tile, heads, n, dim, dtype, below, alike):
+def test_small_weights_of_half_precision(ps, sc, tile, ratio, n, n_req, dim, dtype, below, alike):
     """One token takes nearly all of the weight and its value is 0: the others, 2^-below of it each, make the result.
 
     The bound of check_attention, but for its term of small fp16 weights: the largest weight is 2^10 at
     least, so that one that is subnormal is off by 2^-25 of 2^10 of the sum, T of them by T 2^-35 max|v|;
     and the result is a normal number."""
-    bt, ctx = 16, 4096
+    bt, ctx, kv = 16, 4096, 8
     w = Window([0], [(0, ctx, n)], bt, seed=dim)
+    w.reqs, w.ctx = np.repeat(w.reqs, n_req), np.repeat(w.ctx, n_req)
+    w.row_off, w.n_req, w.n_rows = n * np.arange(n_req + 1, dtype=np.int32), n_req, n * n_req
     g, scale = _gen(dim), dim ** -0.5
-    c = ps.KvCache.empty(w.n_pages, 1, bt, dim, dtype)
-    k, v = (0.0 if alike else 0.02) * _randn(g, ctx, 1, dim), 1.0 + 0.25 * _randn(g, ctx, 1, dim)
+    c = ps.KvCache.empty(w.n_pages, kv, bt, dim, dtype)
+    k, v = (0.0 if alike else 0.02) * _randn(g, ctx, kv, dim), 1.0 + 0.25 * _randn(g, ctx, kv, dim)
     k[0], v[0] = 0.0, 0.0
     k[:, :, 0] = 0.0
     k[0, :, 0] = below * math.log(2.0) / scale / 8.0
     _put(c, "k", w, 0, k)
     _put(c, "v", w, 0, v)
-    q = _randn(g, n, heads, dim)
+    q = _randn(g, w.n_rows, kv * ratio, dim)
     q[..., 0] = 8.0
     q = q.half()
     out, lse = _run(sc, w, c, q)
-    kk, vv = (torch.from_numpy(x)[:, 0] for x in _token_values(c, w, 0, ctx))
+    kk, vv = (torch.from_numpy(x) for x in _token_values(c, w, 0, ctx))
     h = HALF[F16]
-    for j in range(0, n, max(1, n // 8)):
-        m = ctx - n + 1 + j
-        qj = q[j].double().cpu()
-        s = qj @ kk[:m].T.contiguous() * scale
-        big = (qj.abs() @ kk[:m].abs().T.contiguous()).amax(1) * scale
+    for row, head in ((0, 0), (w.n_rows // 2, 3), (w.n_rows - 1, 7)):
+        m, heads = ctx - n + 1 + row % n, slice(head * ratio, (head + 1) * ratio)
+        qj, ks, vs = q[row, heads].double().cpu(), kk[:m, head].contiguous(), vv[:m, head].contiguous()
+        s = qj @ ks.T.contiguous() * scale
+        big = (qj.abs() @ ks.abs().T.contiguous()).amax(1) * scale
         z = torch.logsumexp(s, 1)
         p = torch.exp(s - z[:, None])
-        o, mag = p @ vv[:m], p @ vv[:m].abs()
+        o, mag = p @ vs, p @ vs.abs()
         assert o.abs().min() > 2.0 ** -14
         err = dim * 2.0 ** -24 * big + 2.0 ** -20 + (m / 16 + 16) * 2.0 ** -24
-        off = (out[j].double().cpu() - o).abs()
-        tol = h * o.abs() + (h + 2 * err[:, None]) * (1 + h) * mag + m * 2.0 ** -35 * vv.abs().max()
+        off = (out[row, heads].double().cpu() - o).abs()
+        tol = h * o.abs() + (h + 2 * err[:, None]) * (1 + h) * mag + m * 2.0 ** -35 * vs.abs().max()
         assert (off <= tol).all(), f"off by {(off / tol).max():.1f} times the bound, {(off / o).max():.4f} of the result"
-        off = (lse[j].double().cpu() - z).abs()
+        off = (lse[row, heads].double().cpu() - z).abs()
         assert (off <= err + 2.0 ** -22 * z.abs() + 2.0 ** -22).all()
 
 
