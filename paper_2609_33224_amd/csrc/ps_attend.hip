@@ -1011,9 +1011,10 @@ __global__ __launch_bounds__(64 * (kTall ? kTallWaves : kWideWaves), DP <= 128 ?
   // (scalars throughout: what is loaded after the first store would be a lane's otherwise)
   const AttendHead plan = *a.plan.head;
   const AttendRun run = a.plan.runs[group * kWaves + wave];
-  const int32_t kind = uniform(run.kind), rounds = uniform(run.rounds), number = uniform(run.number);
-  int32_t next = uniform(run.next), at = uniform(run.from), left = uniform(run.units);
-  if (!plan_is_for(plan, a.win, kWaves)) return;
+  // (nothing to do rather than a return, behind which the loads of the run would wait)
+  const int32_t mine = uniform((int32_t)plan_is_for(plan, a.win, kWaves));
+  const int32_t kind = uniform(run.kind), rounds = mine ? uniform(run.rounds) : 0, number = uniform(run.number);
+  int32_t next = uniform(run.next), at = uniform(run.from), left = mine ? uniform(run.units) : 0;
   bool first = true;
   for (int32_t round = 0;;) {
     int32_t k, from, most, piece;

@@ -172,7 +172,9 @@ struct AttendHead {
   int32_t pad;
 };
 __device__ inline bool plan_is_for(const AttendHead& h, const BlockWin& w, int32_t waves) {
-  return h.pages == w.pages && h.pages_len == w.pages_len && h.n_rows == w.n_rows && h.waves == waves;
+  // (one comparison: && would wait for each of its loads in turn)
+  return (((uint64_t)h.pages ^ (uint64_t)w.pages) | (uint64_t)(h.pages_len ^ w.pages_len) |
+          (uint32_t)(h.n_rows ^ w.n_rows) | (uint32_t)(h.waves ^ waves)) == 0;
 }
 
 // What a wave of a workgroup takes: (wide tiles, all waves the same) `rounds` whole
