@@ -575,7 +575,8 @@ ps_status ps_attend_plan_dev(ps_attend_plan* plan, const ps_kv_window* window, u
  * query head h (key / value head h / (n_heads / n_kv_heads)),
  *   out = sum over t in [0, p] of softmax_t(scale * q . k_t) v_t
  * over the request's chain, and lse (float[n_rows * n_heads], may be NULL) the
- * natural logarithm of the sum of exp(scale * q . k_t).  Products take the
+ * natural logarithm of the sum of exp(scale * q . k_t).  scale times log2 e has
+ * to be finite in fp32; it may be 0 or negative.  Products take the
  * operands in q's 16-bit type (PS_T_E4M3 values are converted to it; a 16-bit
  * cache is of q's type), sums and the softmax are in fp32, the softmax's
  * weights are rounded to that type before they multiply v (fp16: a weight of

@@ -203,7 +203,7 @@ struct Piece {
   int32_t ta, tb;
   int32_t slot;  // first row of its partial results, -1: the result itself
   int32_t head;
-  float c;       // |scale| log2 e
+  float c;       // |scale| log2 e, above 0
   uint32_t neg;  // sign bits that turn q where scale is negative
 };
 
@@ -1006,13 +1006,14 @@ __global__ __launch_bounds__(64 * (kTall ? kTallWaves : kWideWaves), DP <= 128 ?
   const float c = a.scale * 1.44269504088896341f;
   Piece p;
   p.head = head;
-  p.c = fmaxf(fabsf(c), 1.17549435e-38f);  // (not 0: it multiplies infinities)
+  p.c = fabsf(c);
   p.neg = c < 0 ? 0x80008000u : 0u;
   // (scalars throughout: what is loaded after the first store would be a lane's otherwise)
   const AttendHead plan = *a.plan.head;
   const AttendRun run = a.plan.runs[group * kWaves + wave];
   // (nothing to do rather than a return, behind which the loads of the run would wait)
   const int32_t mine = uniform((int32_t)plan_is_for(plan, a.win, kWaves));
+
   const int32_t kind = uniform(run.kind), rounds = mine ? uniform(run.rounds) : 0, number = uniform(run.number);
   int32_t next = uniform(run.next), at = uniform(run.from), left = mine ? uniform(run.units) : 0;
   bool first = true;

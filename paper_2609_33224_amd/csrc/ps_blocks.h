@@ -208,6 +208,7 @@ struct AttendPlanDev {
   AttendJoin* joins;
   float* part;        // partial results: [head][slot rows][dim], weights as numerators
   float2* part_ml;    // their maxima (times scale * log2 e) and sums
+  unsigned char* zeros;  // a row of q of a head
   int32_t table_mask;
   int32_t tile_cap[2];
   int32_t slot_rows;  // per head

@@ -141,6 +141,7 @@ hipError_t each_buffer(ps_attend_plan* p, F f) {
   one(d.joins, (size_t)d.slot_rows + rows + d.tile_cap[0]);
   one(d.part, part * p->dim);
   one(d.part_ml, part);
+  one(d.zeros, 2 * PS_MAX_HEAD_DIM);
   return e;
 }
 
@@ -232,6 +233,7 @@ ps_status ps_attend_plan_create(ps_ctx* c, int32_t n_heads, int32_t n_kv_heads, 
   hipError_t e = each_buffer(p, [&](auto*& ptr, size_t bytes) { return c->pool.grow(&ptr, bytes); });
   // (no window's plan: an attention that runs before the first one does nothing)
   if (e == hipSuccess) e = hipMemsetAsync(p->dev.head, 0, sizeof(AttendHead), c->stream);
+  if (e == hipSuccess) e = hipMemsetAsync(p->dev.zeros, 0, 2 * PS_MAX_HEAD_DIM, c->stream);
   if (e == hipSuccess) e = hipStreamSynchronize(c->stream);
   if (e != hipSuccess) {
     release(p);
@@ -280,7 +282,8 @@ ps_status ps_attend_window_dev(ps_attend_plan* p, const ps_kv_cache* cache, cons
   ps_ctx* c = p ? p->ctx : nullptr;
   ps_status st = check_cache(c, cache);
   if (st != PS_OK) return st;
-  if (!std::isfinite(scale)) return fail(c, PS_E_INVAL, "scale is not finite");
+  if (!std::isfinite(scale * 1.44269504088896341f))  // (it multiplies powers of two)
+    return fail(c, PS_E_INVAL, "scale is not finite, or times log2 e it is not");
   const bool none = p && p->planned && (p->win.n_req == 0 || p->win.n_rows == 0);
   if (!none) {
     if ((st = check_rows(c, q, "q", false, cache->head_dim)) != PS_OK ||
@@ -297,6 +300,12 @@ ps_status ps_attend_window_dev(ps_attend_plan* p, const ps_kv_cache* cache, cons
   if (none) return PS_OK;
   DeviceScope ds(c->device);
   AttendArgs a{p->dev, p->win, dev_cache(*cache), dev_rows(*q), dev_rows(*out), lse, scale, p->heads, p->ratio(), 0, 0};
+  if (scale == 0) {
+    // a q of zeros: the kernel's scale multiplies infinities, where scores are masked
+    a.scale = 1;
+    a.q.data = p->dev.zeros;
+    a.q.row = a.q.head = 0;
+  }
   while ((1 << a.bt_shift) < p->bt) ++a.bt_shift;
   a.bt_mul = (uint32_t)(((uint64_t)((1 << a.bt_shift) - p->bt) << 32) / p->bt + 1);
   HIP_TRY(c, ps_launch_attend(a, c->num_cus, (hipStream_t)hip_stream));

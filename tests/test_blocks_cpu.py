@@ -205,3 +205,15 @@ def test_quantiser_of_the_tests():
     assert list(y[0]) == [448, 1.0, 1.25, 2.0 ** -9, 0, 2.0 ** -8, -3.25, 448]
     assert y[1][0] == 224 and np.isnan(y[1][6]) and y[1][7] == -448
     assert REQ.itemsize == 24
+
+
+def test_scales_that_overflow_are_refused(lib):
+    q, cache = _rows(), _cache()
+
+    def go(scale):
+        return lib.ps_attend_window_dev(None, _ref(cache), _ref(q), _ref(q), None, scale, None)
+
+    for s in (3.0e38, -2.4e38):
+        assert go(s) == -1 and "scale" in _err(lib)
+    for s in (2.3e38, -2.3e38, 0.0, 1e-45):
+        assert go(s) == -1 and "plan is NULL" in _err(lib)

@@ -249,3 +249,33 @@ def test_a_plan_that_was_only_captured_is_no_plan_yet(ps, sc):
         p.close()
 
 
+@pytest.mark.parametrize("tile,heads,n", TILES)
+def test_scales_of_zero_and_next_to_it(ps, sc, tile, heads, n):
+    """Products of 2^126 under a scale of 0 are all alike; under 2^-130, a subnormal number, they make scores of 1/16."""
+    bt, ctx, dim = 16, 200, 128
+    w = Window([0], [(0, ctx, n)], bt)
+    g = _gen(1)
+    c = ps.KvCache.empty(w.n_pages, 1, bt, dim, BF16)
+    k = torch.zeros(ctx, 1, dim, device="cuda")
+    k[:, :, 0] = torch.where(torch.arange(ctx, device="cuda") % 2 == 0, 2.0 ** 63, -2.0 ** 63)[:, None]
+    _put(c, "k", w, 0, k)
+    _put(c, "v", w, 0, _randn(g, ctx, 1, dim))
+    q = torch.zeros(n, heads, dim, device="cuda")
+    q[..., 0] = 2.0 ** 63
+    q = q.bfloat16()
+    vv = torch.from_numpy(_token_values(c, w, 0, ctx)[1])[:, 0]
+    h = HALF[BF16]
+    for scale in (0.0, 2.0 ** -130, -2.0 ** -130):
+        out, lse = _run(sc, w, c, q, scale=scale)
+        for j in (0, n - 1):
+            m = ctx - n + 1 + j
+            s = torch.where(torch.arange(m) % 2 == 0, scale * 2.0 ** 126, -scale * 2.0 ** 126).double()
+            z = torch.logsumexp(s, 0)
+            p = torch.exp(s - z)
+            o, mag = p @ vv[:m], p @ vv[:m].abs()
+            # (the scale times log2 e has 18 bits where it is subnormal: a score of 1/16 is off by 2^-22)
+            err = 2.0 ** -20 + (m / 16 + 16) * 2.0 ** -24
+            assert ((out[j].double().cpu() - o).abs() <= h * o.abs() + (h + 2 * err) * (1 + h) * mag).all(), scale
+            assert ((lse[j].double().cpu() - z).abs() <= err + 2.0 ** -22 * z.abs() + 2.0 ** -22).all(), scale
+
+
