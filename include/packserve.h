@@ -506,7 +506,8 @@ typedef struct {
 
 /* Rows of heads: element e of head h of row i is data[i * row_stride +
  * h * head_stride + e] (strides in elements, multiples of 8; data 16-byte
- * aligned; PS_T_BF16 or PS_T_F16). */
+ * aligned; PS_T_BF16 or PS_T_F16).  Rows and heads that a call writes must not
+ * share elements (both strides are head_dim at least, PS_E_INVAL otherwise). */
 typedef struct {
   void* data;
   int64_t row_stride, head_stride;

@@ -64,14 +64,31 @@ ps_status check_window(ps_ctx* c, const ps_kv_window* w) {
   return PS_OK;
 }
 
-ps_status check_rows(ps_ctx* c, const ps_rows* r, const char* what, bool written, int32_t dim) {
+// Whether two of n_rows x heads runs of dim elements share an element: two that are dr rows and dh heads
+// apart do where |dr row_stride + dh head_stride| < dim.
+bool rows_overlap(const ps_rows& r, int64_t n_rows, int32_t heads, int32_t dim) {
+  const int64_t rs = r.row_stride, hs = r.head_stride;
+  if ((n_rows > 1 && rs < dim) || (heads > 1 && hs < dim)) return true;
+  if (n_rows <= 1 || heads <= 1) return false;
+  // a row's heads between its start and the next one's, or a head's rows likewise
+  if (rs >= (heads - 1) * hs + dim || hs >= (n_rows - 1) * rs + dim) return false;
+  for (int64_t dh = 1; dh < heads; ++dh) {
+    const int64_t dr = dh * hs / rs;  // as many rows back, or one more
+    if ((dr < n_rows && dh * hs - dr * rs < dim) || (dr + 1 < n_rows && (dr + 1) * rs - dh * hs < dim)) return true;
+  }
+  return false;
+}
+
+// written: n_rows rows of `heads` heads are (none where that is not known yet).
+ps_status check_rows(ps_ctx* c, const ps_rows* r, const char* what, bool written, int64_t n_rows, int32_t heads,
+                     int32_t dim) {
   if (!r || !r->data) return fail(c, PS_E_INVAL, "%s is NULL", what);
   if (r->dtype != PS_T_BF16 && r->dtype != PS_T_F16) return fail(c, PS_E_INVAL, "%s is not of a 16-bit type", what);
   if (!aligned16(r->data)) return fail(c, PS_E_INVAL, "%s is not 16-byte aligned", what);
   if (r->row_stride % 8 || r->head_stride % 8 || r->row_stride < 0 || r->head_stride < 0 ||
       r->row_stride > (int64_t)1 << 40 || r->head_stride > (int64_t)1 << 40)
     return fail(c, PS_E_INVAL, "strides of %s are not multiples of 8 in [0, 2^40]", what);
-  if (written && (r->row_stride < dim || r->head_stride < dim))
+  if (written && (r->row_stride < dim || r->head_stride < dim || rows_overlap(*r, n_rows, heads, dim)))
     return fail(c, PS_E_INVAL, "rows of %s overlap", what);
   return PS_OK;
 }
@@ -96,8 +113,8 @@ ps_status kv_rows(ps_ctx* c, bool write, const ps_kv_cache* cache, const ps_kv_w
   if (w->n_pages > cache->n_pages) return fail(c, PS_E_INVAL, "the window names more pages than the cache has");
   const bool none = w->n_req == 0 || w->n_rows == 0;
   if (!none) {
-    if ((st = check_rows(c, k, "k", !write, cache->head_dim)) != PS_OK ||
-        (st = check_rows(c, v, "v", !write, cache->head_dim)) != PS_OK)
+    if ((st = check_rows(c, k, "k", !write, w->n_rows, cache->n_kv_heads, cache->head_dim)) != PS_OK ||
+        (st = check_rows(c, v, "v", !write, w->n_rows, cache->n_kv_heads, cache->head_dim)) != PS_OK)
       return st;
     if (k->dtype != v->dtype || (cache->dtype != PS_T_E4M3 && k->dtype != cache->dtype))
       return fail(c, PS_E_INVAL, "k, v and the cache differ in type");
@@ -286,8 +303,8 @@ ps_status ps_attend_window_dev(ps_attend_plan* p, const ps_kv_cache* cache, cons
     return fail(c, PS_E_INVAL, "scale is not finite, or times log2 e it is not");
   const bool none = p && p->planned && (p->win.n_req == 0 || p->win.n_rows == 0);
   if (!none) {
-    if ((st = check_rows(c, q, "q", false, cache->head_dim)) != PS_OK ||
-        (st = check_rows(c, out, "out", true, cache->head_dim)) != PS_OK)
+    if ((st = check_rows(c, q, "q", false, 0, 0, cache->head_dim)) != PS_OK ||
+        (st = check_rows(c, out, "out", true, p ? p->win.n_rows : 0, p ? p->heads : 0, cache->head_dim)) != PS_OK)
       return st;
     if (q->dtype != out->dtype || (cache->dtype != PS_T_E4M3 && q->dtype != cache->dtype))
       return fail(c, PS_E_INVAL, "q, out and the cache differ in type");
@@ -310,6 +327,11 @@ ps_status ps_attend_window_dev(ps_attend_plan* p, const ps_kv_cache* cache, cons
   a.bt_mul = (uint32_t)(((uint64_t)((1 << a.bt_shift) - p->bt) << 32) / p->bt + 1);
   HIP_TRY(c, ps_launch_attend(a, c->num_cus, (hipStream_t)hip_stream));
   return PS_OK;
+}
+
+// For the tests (not in packserve.h): the check of rows that are written.
+int32_t ps_test_rows_overlap(const ps_rows* r, int64_t n_rows, int32_t heads, int32_t dim) {
+  return rows_overlap(*r, n_rows, heads, dim);
 }
 
 // For the tests (not in packserve.h): where the cache calls look for a row, by

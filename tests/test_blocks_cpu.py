@@ -217,3 +217,33 @@ def test_scales_that_overflow_are_refused(lib):
         assert go(s) == -1 and "scale" in _err(lib)
     for s in (2.3e38, -2.3e38, 0.0, 1e-45):
         assert go(s) == -1 and "plan is NULL" in _err(lib)
+
+
+def test_rows_that_would_be_written_over_each_other(lib):
+    """Against every pair of rows and heads; and the read call refuses what the check finds."""
+    f = lib.ps_test_rows_overlap
+    f.argtypes = [ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32]
+    f.restype = ctypes.c_int32
+    rng = np.random.default_rng(0)
+    found = [0, 0]
+    for _ in range(4000):
+        n, heads, dim = int(rng.integers(1, 7)), int(rng.integers(1, 6)), 16 * int(rng.integers(1, 4))
+        rs, hs = (8 * int(x) for x in rng.integers(0, 40, 2))
+        at = np.sort((np.arange(n)[:, None] * rs + np.arange(heads)[None] * hs).reshape(-1))
+        want = bool((np.diff(at) < dim).any())
+        assert bool(f(ctypes.byref(_rows(row_stride=rs, head_stride=hs)), n, heads, dim)) == want, (n, heads, dim, rs, hs)
+        found[want] += 1
+    assert min(found) > 500
+    # (1 << 20) rows of 128 heads
+    big = lambda rs, hs, n=1 << 20, h=128: f(ctypes.byref(_rows(row_stride=rs, head_stride=hs)), n, h, 128)  # noqa: E731
+    assert not big(128 * 128, 128) and not big(128, 128 << 20) and big(128 * 127, 128) and big(128, (128 << 20) - 8)
+
+    def read(**kw):
+        k = _rows(**kw)
+        code = lib.ps_kv_read_dev(None, _ref(_cache()), _ref(_window(n_rows=4)), _ref(k), _ref(_rows()), None)
+        return code, _err(lib)
+
+    assert read(row_stride=64, head_stride=64)[0] == -1 and "overlap" in read(row_stride=64, head_stride=64)[1]
+    for kw in (dict(row_stride=128, head_stride=64), dict(row_stride=64, head_stride=256),
+               dict(row_stride=64 * 3, head_stride=64 * 2)):
+        assert "ctx is NULL" in read(**kw)[1], kw
