@@ -541,12 +541,13 @@ ps_status ps_kv_read_dev(ps_ctx* ctx, const ps_kv_cache* cache, const ps_kv_wind
 
 /*
  * A plan: how the attention of one window is cut into work, and the memory
- * for it (from the context; freed by ps_attend_plan_destroy, or with the
+ * for it (the context's; freed by ps_attend_plan_destroy, or with the
  * context).  It serves windows of at most max_req requests and max_rows rows
  * with n_heads query heads over n_kv_heads (a divisor of n_heads) and the
- * given head_dim and block_tokens.  A plan is destroyed, or its context is,
- * once the work that uses it is done and no graph that holds it will run
- * again: its memory goes to the context's next buffers.
+ * given head_dim and block_tokens.  ps_attend_plan_destroy waits for the
+ * device's work and gives the memory back to the device, also while a stream is
+ * being captured (whose work it leaves alone).  No graph that holds the plan may
+ * run afterwards.
  */
 typedef struct ps_attend_plan ps_attend_plan;
 ps_status ps_attend_plan_create(ps_ctx* ctx, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,

@@ -473,7 +473,9 @@ def ps_kv_read_dev(ctx, cache: KvCache, window: KvWindow, k: torch.Tensor, v: to
 class AttendPlan:
     """Attention of windows over a block cache: build_dev plans a window,
     attend_dev runs the attention of one layer (any number of times).  Keeps
-    its context (a Scorer) alive."""
+    its context (a Scorer) alive.  close(), or the last reference to it going,
+    waits for the device and frees the plan's memory: keep it as long as a
+    captured graph that holds it may run."""
 
     def __init__(self, scorer: "Scorer", n_heads: int, n_kv_heads: int, head_dim: int, block_tokens: int,
                  max_req: int, max_rows: int):

@@ -266,12 +266,16 @@ ps_status ps_attend_plan_create(ps_ctx* c, int32_t n_heads, int32_t n_kv_heads, 
 ps_status ps_attend_plan_destroy(ps_attend_plan* p) {
   if (!p) return PS_OK;
   DeviceScope ds(p->ctx->device);
+  // (freeing is refused to a thread that captures, and ends the capture, unless it says that it may)
+  hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
+  const bool relaxed = hipThreadExchangeStreamCaptureMode(&mode) == hipSuccess;
   for (ps_attend_plan** at = &p->ctx->plans; *at; at = &(*at)->next)
     if (*at == p) {
       *at = p->next;
       break;
     }
   release(p);
+  if (relaxed) (void)hipThreadExchangeStreamCaptureMode(&mode);
   delete p;
   return PS_OK;
 }

@@ -279,3 +279,43 @@ def test_scales_of_zero_and_next_to_it(ps, sc, tile, heads, n):
             assert ((lse[j].double().cpu() - z).abs() <= err + 2.0 ** -22 * z.abs() + 2.0 ** -22).all(), scale
 
 
+def test_a_plan_goes_while_a_stream_is_captured(ps, sc):
+    """As Python's collector may have it: the capture goes on, and the memory is back.  Work on another stream that
+    still uses the plan is waited for."""
+    from tests.gpu_util import limit_memory
+    heads, kv, dim, bt = 8, 2, 128, 16
+    w = Window([20], [(0, 320 + 9 * k, 1) for k in range(9)], bt)
+    win, c = w.dev(), ps.KvCache.empty(w.n_pages, kv, bt, dim, BF16)
+    for name in "kv":
+        for r in range(w.n_req):
+            _put(c, name, w, r, _randn(_gen(r), int(w.ctx[r]), kv, dim))
+    q = _randn(_gen(1), w.n_rows, heads, dim).bfloat16()
+    ref, _ = _run(sc, w, c, q)
+    s = ps.Scorer(0)
+    p = s.attend_plan(heads, kv, dim, bt, w.n_req, w.n_rows)
+    p.build_dev(win)
+    held = limit_memory(s, 0)
+    other = s.attend_plan(heads, kv, dim, bt, w.n_req, w.n_rows)
+    outs = [torch.zeros_like(q) for _ in range(41)]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        p.attend_dev(c, q, outs[0])
+        with torch.cuda.stream(side):
+            other.build_dev(win)
+            for out in outs[1:]:
+                other.attend_dev(c, q, out)
+        del other
+    assert limit_memory(s, 0) == held
+    torch.cuda.synchronize()
+    assert all(torch.equal(out, ref) for out in outs[1:])
+    for _ in range(3):
+        outs[0].zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], ref)
+    p.close()
+    s.close()
+
+
