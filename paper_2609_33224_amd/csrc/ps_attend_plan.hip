@@ -389,11 +389,26 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
     const int32_t n_wide = wide_groups;
     const bool mine = tid < n_wide;
     int64_t whole = 0, total, share = 0;
-    for (rounds = n_tiles[0] / n_wide;; --rounds) {
-      whole = 0;
-      for (int32_t i = 0; mine && i < rounds; ++i) whole += units_of(p.tiles[0][tile_of_round(tid, i, n_wide)]) + kTileUnits;
-      if (!__syncthreads_or(mine && rounds > 0 && whole * n_wide > units[0])) break;
+    auto tile_at = [&](int32_t i) { return units_of(p.tiles[0][tile_of_round(tid, i, n_wide)]) + kTileUnits; };
+    // (each takes as many as it can, in one pass, and gives back what the others cannot.  Rounds taken
+    // off one by one, all summed anew, were 16.8 ms for 2047 tiles of each of 128 heads behind one of
+    // 400,000 positions)
+    const int32_t most = n_tiles[0] / n_wide;
+    int32_t can = 0;
+    int64_t sum = 0;
+    for (int32_t i = 0; mine && i < most; ++i) {
+      sum += tile_at(i);
+      if (sum * n_wide <= units[0]) {
+        can = i + 1;
+        whole = sum;
+      }
     }
+    if (tid == 0) n_todo = most;
+    __syncthreads();
+    if (mine && can < most) atomicMin(&n_todo, can);
+    __syncthreads();
+    rounds = n_todo;
+    for (int32_t i = rounds; mine && i < can; ++i) whole -= tile_at(i);
     // a level that those below it are filled up to
     int64_t left = units[0], n_below = n_wide;
     bool below = mine;

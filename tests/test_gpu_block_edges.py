@@ -319,3 +319,28 @@ def test_a_plan_goes_while_a_stream_is_captured(ps, sc):
     s.close()
 
 
+def test_a_plan_of_many_tiles_behind_a_long_one(ps, sc):
+    """Thousands of tiles a head, one of the first of which is more than a workgroup's share: the plan is made in
+    about the time that a window without that one takes."""
+    heads, dim, bt, n = 128, 16, 64, 2047
+    took = []
+    for ctx in (128, 400_000):
+        w = Window([0], [(0, 128, 128)] * n, bt)
+        w.n_pages, w.pages = 4, np.concatenate([w.pages % 4, np.zeros(-(-ctx // bt), np.int32)])
+        w.reqs[0] = (0, len(w.pages) - -(-ctx // bt), 0, -(-ctx // bt))
+        w.ctx[0] = ctx
+        p, win = sc.attend_plan(heads, heads, dim, bt, w.n_req, w.n_rows), w.dev()
+        times = []
+        for _ in range(4):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            torch.cuda.synchronize()
+            a.record()
+            p.build_dev(win)
+            b.record()
+            b.synchronize()
+            times.append(a.elapsed_time(b))
+        took.append(min(times[1:]))
+    # (checking 6,250 pages and cutting one long tile are less than the second window's own work)
+    assert took[1] <= 3 * took[0], took
+
+
