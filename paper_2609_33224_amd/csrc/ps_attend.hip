@@ -293,7 +293,7 @@ constexpr int narrow_positions(bool kQ8, int DP) { return kQ8 && DP <= 128 ? 64 
 // selects in it, chunks of full heads took 2.5% longer.)  The least such head:
 constexpr int least_dim(int DP) { return DP == 64 ? 16 : DP / 2 + 16; }
 
-template <bool kF16, bool kQ8, int DP, bool kPad, int RB>
+template <bool kF16, bool kQ8, int DP, bool kPad>
 __device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char* vs) {
   constexpr int kTok = narrow_positions(kQ8, DP);
   constexpr int kH = kTok / 16;                       // rows of positions in the first product
@@ -302,18 +302,14 @@ __device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char*
   constexpr int kLoads = kQ8 ? DP / 64 : DP / 32;     // 16-byte loads per lane and 16 positions
   constexpr int kDB = DP / 16;                        // blocks of the second product
   constexpr int kV = narrow_stride(DP);
+  static_assert(kNarrowRows == 16, "a row of the tile per column of the products");
   const int lane = fresh(threadIdx.x & 63), col = lane & 15, g = lane >> 4;
   const int D = a.cache.dim;
 
-  f32x4 acc[RB][kDB];
-  float m[RB], l[RB];  // (the maximum of scores times c, less weight_lift)
+  f32x4 acc[kDB];
+  float m = -INFINITY, l = 0;  // (the maximum of scores times c, less weight_lift)
 #pragma unroll
-  for (int b = 0; b < RB; ++b) {
-    m[b] = -INFINITY;
-    l[b] = 0;
-#pragma unroll
-    for (int k = 0; k < kDB; ++k) acc[b][k] = f32x4{0, 0, 0, 0};
-  }
+  for (int k = 0; k < kDB; ++k) acc[k] = f32x4{0, 0, 0, 0};
 
   const int32_t last = p.tb - 1;
   uint32_t page[kH];
@@ -344,29 +340,20 @@ __device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char*
   };
 
   // Pages and rows are asked for together, then keys and values, then q: loads return
-    // in order, so that a wait for q's would hold the others back.
-  u32x4 q[RB][kSteps];
-  int32_t lim[RB], least = INT32_MAX;
-  int64_t qat[RB];
+  // in order, so that a wait for q's would hold the others back.
+  u32x4 q[kSteps];
   pages(p.ta);
-#pragma unroll
-  for (int b = 0; b < RB; ++b) {
-    const int32_t r = b * 16 + col;
-    const RowAt at = row_at(a, p, min(r, p.rows - 1));
-    lim[b] = a.plan.lim[at.place];
-    qat[b] = a.plan.row[at.place] * a.q.row + (int64_t)at.head * a.q.head;
-  }
+  const RowAt qrow = row_at(a, p, min(col, p.rows - 1));
+  int32_t lim = a.plan.lim[qrow.place];
+  const int64_t qat = a.plan.row[qrow.place] * a.q.row + (int64_t)qrow.head * a.q.head;
   loads(p.ta);
   pages(p.ta + kTok);
+  const bool has = col < p.rows;
 #pragma unroll
-  for (int b = 0; b < RB; ++b) {
-    const bool has = b * 16 + col < p.rows;
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s)
-      q[b][s] = load_q(a, p, qat[b], has, kQ8 ? 64 * (s >> 1) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g);
-    if (!has) lim[b] = INT32_MAX;
-    least = min(least, lim[b]);
-  }
+  for (int s = 0; s < kSteps; ++s)
+    q[s] = load_q(a, p, qat, has, kQ8 ? 64 * (s >> 1) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g);
+  if (!has) lim = INT32_MAX;
+  int32_t least = lim;
   for (int o = 8; o > 0; o >>= 1) least = min(least, __shfl_xor(least, o, 64));
 
   for (int32_t t = p.ta; t < p.tb; t += kTok) {
@@ -401,12 +388,11 @@ __device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char*
 #pragma unroll
           for (int h = 0; h < kH; ++h) kr[h][i] = u32x4{0, 0, 0, 0};
     }
-    // scores: position 16 h + 4 g + i of the step, row b * 16 + col
-    f32x4 s[RB][kH];
+    // scores: position 16 h + 4 g + i of the step, row col
+    f32x4 s[kH];
 #pragma unroll
     for (int h = 0; h < kH; ++h) {
-#pragma unroll
-      for (int b = 0; b < RB; ++b) s[b][h] = f32x4{0, 0, 0, 0};
+      s[h] = f32x4{0, 0, 0, 0};
 #pragma unroll
       for (int st = 0; st < kSteps; ++st) {
         u32x4 ka;
@@ -416,8 +402,7 @@ __device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char*
         } else {
           ka = kr[h][st % kLoads];
         }
-#pragma unroll
-        for (int b = 0; b < RB; ++b) s[b][h] = mfma16<kF16>(ka, q[b][st], s[b][h]);
+        s[h] = mfma16<kF16>(ka, q[st], s[h]);
       }
     }
     // (behind the last step too, its last position over: of loads that depend on a branch
@@ -429,32 +414,26 @@ __device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char*
 
     if (masked) {
 #pragma unroll
-      for (int b = 0; b < RB; ++b)
+      for (int h = 0; h < kH; ++h)
 #pragma unroll
-        for (int h = 0; h < kH; ++h)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (t + 16 * h + 4 * g + i >= min(lim[b], p.tb)) s[b][h][i] = -INFINITY;
+        for (int i = 0; i < 4; ++i)
+          if (t + 16 * h + 4 * g + i >= min(lim, p.tb)) s[h][i] = -INFINITY;
     }
-    float mc[RB];
+    float top = s[0][0];
 #pragma unroll
-    for (int b = 0; b < RB; ++b) {
-      float top = s[b][0][0];
+    for (int i = 1; i < 4 * kH; ++i) top = fmaxf(top, s[i >> 2][i & 3]);
+    top = fmaxf(top, __shfl_xor(top, 16, 64));
+    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    // (kept as the rounded product that the weights take, so that the factor of a maximum that has
+    // not moved is 1: a fused m c - mc is the product's rounding error, the same in every step, and
+    // bent the sums of 1024 steps under scores of 100 to 200 by 4e-3)
+    const float nm = fmaxf(m, top * p.c - weight_lift(kF16));
+    const float mc = nm == -INFINITY ? 0.0f : nm;
+    const float f = __builtin_amdgcn_exp2f(m - mc);
+    m = nm;
+    l *= f;
 #pragma unroll
-      for (int i = 1; i < 4 * kH; ++i) top = fmaxf(top, s[b][i >> 2][i & 3]);
-      top = fmaxf(top, __shfl_xor(top, 16, 64));
-      top = fmaxf(top, __shfl_xor(top, 32, 64));
-      // (kept as the rounded product that the weights take, so that the factor of a maximum that has
-      // not moved is 1: a fused m c - mc is the product's rounding error, the same in every step, and
-      // bent the sums of 1024 steps under scores of 100 to 200 by 4e-3)
-      const float nm = fmaxf(m[b], top * p.c - weight_lift(kF16));
-      mc[b] = nm == -INFINITY ? 0.0f : nm;
-      const float f = __builtin_amdgcn_exp2f(m[b] - mc[b]);
-      m[b] = nm;
-      l[b] *= f;
-#pragma unroll
-      for (int k = 0; k < kDB; ++k) acc[b][k] *= f;
-    }
+    for (int k = 0; k < kDB; ++k) acc[k] *= f;
     if (masked && __any(odd != 0))
 #pragma unroll 1
       for (int32_t o = t; o < min(t + kTok, p.tb); ++o)
@@ -462,9 +441,7 @@ __device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char*
         for (int k = 0; k < kDB; ++k) {
           const f32x4 x = odd_values<kF16, kQ8>(a, p, o, min(16 * k + fresh(4 * g), D - 4));
 #pragma unroll
-          for (int b = 0; b < RB; ++b)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[b][k][i] = added(acc[b][k][i], o < lim[b] ? x[i] : 0.0f);
+          for (int i = 0; i < 4; ++i) acc[k][i] = added(acc[k][i], o < lim ? x[i] : 0.0f);
         }
     // lane i of 16: row 4 g + i / 4, elements 16 k + 4 (i % 4) ..
     auto turned = [&](int x, int k) {
@@ -475,41 +452,34 @@ __device__ void narrow_piece(const AttendArgs& a, const Piece& p, unsigned char*
     };
 #pragma unroll
     for (int x = 0; x < kX; ++x) {
-      u32x4 va[kDB], pr[RB];
+      u32x4 va[kDB], pr;
 #pragma unroll
       for (int k = 0; DP <= 128 && k < kDB; ++k) va[k] = turned(x, k);
 #pragma unroll
-      for (int b = 0; b < RB; ++b) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const f32x4& v = s[b][2 * x + (i >> 1)];
-          const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(v[(2 * i) & 3], p.c, -mc[b]));
-          const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(v[(2 * i + 1) & 3], p.c, -mc[b]));
-          l[b] += e0 + e1;
-          pr[b][i] = pack<kF16>(e0, e1);
-        }
+      for (int i = 0; i < 4; ++i) {
+        const f32x4& v = s[2 * x + (i >> 1)];
+        const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(v[(2 * i) & 3], p.c, -mc));
+        const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(v[(2 * i + 1) & 3], p.c, -mc));
+        l += e0 + e1;
+        pr[i] = pack<kF16>(e0, e1);
       }
 #pragma unroll
       for (int k = 0; k < kDB; ++k) {
         if (DP > 128) va[0] = turned(x, k);  // (no registers to read ahead)
-#pragma unroll
-        for (int b = 0; b < RB; ++b) acc[b][k] = mfma16<kF16>(va[DP > 128 ? 0 : k], pr[b], acc[b][k]);
+        acc[k] = mfma16<kF16>(va[DP > 128 ? 0 : k], pr, acc[k]);
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
 
   const int at = fresh(lane), d0 = 4 * (at >> 4);
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+  const int32_t r = at & 15;
+  if (r < p.rows) {
+    const float inv = put_ml<kF16>(a, p, r, m, l, d0 == 0);
 #pragma unroll
-  for (int b = 0; b < RB; ++b) {
-    l[b] += __shfl_xor(l[b], 16, 64);
-    l[b] += __shfl_xor(l[b], 32, 64);
-    const int32_t r = b * 16 + (at & 15);
-    if (r < p.rows) {
-      const float inv = put_ml<kF16>(a, p, r, m[b], l[b], d0 == 0);
-#pragma unroll
-      for (int k = 0; k < kDB; ++k) put4<kF16>(a, p, r, 16 * k + d0, acc[b][k], inv);
-    }
+    for (int k = 0; k < kDB; ++k) put4<kF16>(a, p, r, 16 * k + d0, acc[k], inv);
   }
 }
 
@@ -1054,7 +1024,7 @@ __global__ __launch_bounds__(64 * (kTall ? kTallWaves : kWideWaves), DP <= 128 ?
       else if (kind == 0) wide_piece<kF16, kQ8, DP, kPad, 1>(a, p, smem, odd_at);
     }
     if (kind == 1)
-      narrow_piece<kF16, kQ8, DP, kPad, kNarrowRows / 16>(a, p, smem + wave * narrow_positions(kQ8, DP) * narrow_stride(DP));
+      narrow_piece<kF16, kQ8, DP, kPad>(a, p, smem + wave * narrow_positions(kQ8, DP) * narrow_stride(DP));
     if (most != INT32_MAX) left -= n;
   }
 }
