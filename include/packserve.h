@@ -520,9 +520,12 @@ typedef struct {
  * head: with m its largest finite magnitude, x - 127 is the least exponent e
  * in [-126, 127] with m <= 448 * 2^e, and an element is rounded once, to the
  * nearest even multiple, as element * 2^-e; infinities become +-448, NaN stays
- * NaN.  Rows without a token, of a malformed request (see
- * ps_attend_plan_dev) or in a page outside [0, window.n_pages) are not written;
- * nor are other slots of the pages.  Rows that name the same slot (one page
+ * NaN.  Not written are rows without a token, rows in a page outside
+ * [0, window.n_pages), rows of a request whose segments or ctx_tok are malformed
+ * (as ps_attend_plan_dev says; a bad page elsewhere in its chain, which that
+ * call flags too, does not matter here), and other slots of the pages.  Where
+ * row_off does not ascend, a row is written as a row of one request whose range
+ * holds it, or not at all.  Rows that name the same slot (one page
  * in two chains) must hold the same values.  Asynchronous on `hip_stream`; no
  * allocation, so it can be captured.  PS_E_INVAL / PS_E_RANGE, before any
  * launch, for a NULL, misaligned or mismatched argument.
@@ -532,9 +535,11 @@ ps_status ps_kv_write_dev(ps_ctx* ctx, const ps_kv_cache* cache, const ps_kv_win
 
 /*
  * Read the window's rows back: the cache's values, for PS_T_E4M3 rounded to
- * the rows' 16-bit type (exact unless the product leaves its normal range).
+ * the rows' 16-bit type (exact unless the product leaves its normal range: fp16
+ * rows of magnitudes from 63488 on are stored as 65536, an infinity in fp16).
  * Rows of a request that have no token, or that ps_kv_write_dev would not
- * write, are set to zero.  Otherwise as ps_kv_write_dev.
+ * write, are set to zero.  k and v must not overlap.  Otherwise as
+ * ps_kv_write_dev.
  */
 ps_status ps_kv_read_dev(ps_ctx* ctx, const ps_kv_cache* cache, const ps_kv_window* window,
                          const ps_rows* k, const ps_rows* v, void* hip_stream);
@@ -578,12 +583,13 @@ ps_status ps_attend_plan_dev(ps_attend_plan* plan, const ps_kv_window* window, u
  *   out = sum over t in [0, p] of softmax_t(scale * q . k_t) v_t
  * over the request's chain, and lse (float[n_rows * n_heads], may be NULL) the
  * natural logarithm of the sum of exp(scale * q . k_t).  scale times log2 e has
- * to be finite in fp32; it may be 0 or negative.  Products take the
- * operands in q's 16-bit type (PS_T_E4M3 values are converted to it; a 16-bit
- * cache is of q's type), sums and the softmax are in fp32, the softmax's
- * weights are rounded to that type before they multiply v (fp16: a weight of
- * less than 2^-24 of the row's largest loses bits, and is off by 2^-35 of it
- * at most).  A row without a token gives zeros and -inf.  What lies in the pages behind a row's position
+ * to be finite in fp32; it may be 0 or negative.  Products take the operands in
+ * q's 16-bit type (PS_T_E4M3 values are converted to it as ps_kv_read_dev does,
+ * so they are within fp16's range where q is fp16; a 16-bit cache is of q's
+ * type), sums and the softmax are in fp32, the softmax's weights are rounded to
+ * that type before they multiply v (fp16: a weight of less than 2^-24 of the
+ * row's largest loses bits, and is off by 2^-35 of it at most).  A row without a
+ * token gives zeros and -inf.  What lies in the pages behind a row's position
  * does not reach it, whatever its bits.  Results do not depend on the run: the
  * same window gives the same bits.  out must not overlap q or the cache.
  * Asynchronous on `hip_stream`, no allocation.  The plan's memory is in use

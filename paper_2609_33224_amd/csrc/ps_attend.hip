@@ -1167,6 +1167,7 @@ int32_t ps_attend_per_cu(int32_t dim, bool tall) { return dim <= 128 && !tall ? 
 // 8 (4 rows a token), e4m3, wide and tall: 8 requests of 700 new tokens behind 16384 1728 and 1451
 // us, 4 of 512 702 and 581; 4 of 2048 behind 2048 536 and 461, behind none 222 and 206; 16 of 512
 // behind none 101 and 114, 24 of 16 to 1500 244 and 259.  (8 heads over 8: 8 of 512 behind 16384 355 and 296.)
+// A mean: requests that decode beside a chunk, and those of no rows that pad a window, bring it down.
 constexpr int kTallMin = 1024;
 bool ps_attend_tall(int32_t dim, int64_t rows, int32_t n_req) {
   return dim > 64 && dim <= 128 && rows >= (int64_t)kTallMin * n_req;
