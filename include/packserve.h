@@ -595,10 +595,10 @@ ps_status ps_attend_plan_dev(ps_attend_plan* plan, const ps_kv_window* window, u
  * Asynchronous on `hip_stream`, no allocation.  The plan's memory is in use
  * until the work is done: calls on one plan must not overlap (two graphs that
  * may run at the same time need a plan each).  PS_E_STATE before
- * ps_attend_plan_dev.  It runs on the plan that the memory holds by then, of
- * this call's window: with a plan for another pages buffer, pages_len or n_rows
- * (planned, or replayed, since this call was made or captured) it does nothing
- * and leaves out as it was, and with one for another n_req it may.
+ * ps_attend_plan_dev.  It runs on the plan that the plan's memory holds by then.
+ * With one for another pages buffer or more rows than this call was made or
+ * captured with (a window planned, or a graph replayed, since then) it does
+ * nothing and leaves out as it was; with one for another n_req or n_rows it may.
  */
 ps_status ps_attend_window_dev(ps_attend_plan* plan, const ps_kv_cache* cache, const ps_rows* q,
                                const ps_rows* out, float* lse, float scale, void* hip_stream);

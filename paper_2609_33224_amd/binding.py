@@ -475,7 +475,8 @@ class AttendPlan:
     attend_dev runs the attention of one layer (any number of times).  Keeps
     its context (a Scorer) alive.  close(), or the last reference to it going,
     waits for the device and frees the plan's memory: keep it as long as a
-    captured graph that holds it may run."""
+    captured graph that holds it may run.  After a graph has planned another
+    window, build_dev comes before the next attend_dev."""
 
     def __init__(self, scorer: "Scorer", n_heads: int, n_kv_heads: int, head_dim: int, block_tokens: int,
                  max_req: int, max_rows: int):

@@ -155,7 +155,7 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
   if (__syncthreads_or(bad)) {
     if (d_flags)
       for (int32_t r = tid; r < n; r += kThreads) d_flags[r] = PS_R_INVALID;
-    if (tid == 0) *p.head = AttendHead{w.pages, w.pages_len, w.n_rows, p.waves, 0, 0};
+    if (tid == 0) *p.head = AttendHead{w.pages, w.n_rows, p.waves, 0, {}};
     for (int32_t x = tid; x < p.n_runs; x += kThreads) p.runs[x].rounds = p.runs[x].units = 0;
     return;
   }
@@ -569,7 +569,7 @@ __global__ __launch_bounds__(kThreads) void plan_cut_kernel(AttendPlanDev p, Blo
         push(s.p0 + j, -1, nullptr, -1, 0);
   }
   __syncthreads();
-  if (tid == 0) *p.head = AttendHead{w.pages, w.pages_len, w.n_rows, p.waves, n_todo, 0};
+  if (tid == 0) *p.head = AttendHead{w.pages, w.n_rows, p.waves, n_todo, {}};
 }
 
 }  // namespace

@@ -161,20 +161,18 @@ struct alignas(16) AttendJoin {
 };
 
 // What the plan was made for.  An attention that was captured alone runs on whatever plan its memory
-// holds when it is replayed: one for other workgroups or another window's pages and rows, whose
-// offsets and rows may lie behind this one's buffers, is not run.
+// holds when it is replayed: one for other workgroups, for another buffer of pages, behind whose
+// end its offsets may lie, or for more rows than this call's buffers have, is not run.
 struct AttendHead {
   const int32_t* pages;
-  int64_t pages_len;
   int32_t n_rows;
   int32_t waves;  // AttendPlanDev::waves when the plan was made
   int32_t n_joins;
-  int32_t pad;
+  int32_t pad[3];
 };
 __device__ inline bool plan_is_for(const AttendHead& h, const BlockWin& w, int32_t waves) {
   // (one comparison: && would wait for each of its loads in turn)
-  return (((uint64_t)h.pages ^ (uint64_t)w.pages) | (uint64_t)(h.pages_len ^ w.pages_len) |
-          (uint32_t)(h.n_rows ^ w.n_rows) | (uint32_t)(h.waves ^ waves)) == 0;
+  return (((uint64_t)h.pages ^ (uint64_t)w.pages) | (uint32_t)(h.waves ^ waves) | (uint32_t)(h.n_rows > w.n_rows)) == 0;
 }
 
 // What a wave of a workgroup takes: (wide tiles, all waves the same) `rounds` whole

@@ -227,6 +227,37 @@ def test_attention_captured_alone_runs_on_its_own_windows_plan_only(ps, sc):
         assert torch.equal(out, ref) and torch.equal(lse, lref)
 
 
+def test_attention_captured_alone_takes_windows_in_the_same_buffers(ps, sc):
+    """More pages named behind the ones that were, fewer rows and requests."""
+    heads, kv, dim, bt, n = 8, 2, 64, 16, 6
+    w = Window([2, 5], [(k % 2, 100 + 9 * k, 1) for k in range(n)], bt)
+    c = ps.KvCache.empty(w.n_pages, kv, bt, dim, BF16)
+    for name in "kv":
+        for r in range(n):
+            _put(c, name, w, r, _randn(_gen(r % 2), int(w.ctx[r]), kv, dim))
+    q, out = _randn(_gen(1), n, heads, dim).bfloat16(), torch.zeros(n, heads, dim, dtype=BF16, device="cuda")
+    pages, reqs, ctx, off = w.dev().tensors
+    two = int(w.reqs["tail_off"][2])
+    first = ps.KvWindow(pages[:two], reqs, ctx, off, 2, 2, w.n_pages)
+    whole = ps.KvWindow(pages, reqs, ctx, off, n, n, w.n_pages)
+    p = sc.attend_plan(heads, kv, dim, bt, n, n)
+    p.build_dev(whole)
+    p.attend_dev(c, q, out)
+    ref = out.clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        p.attend_dev(c, q, out)
+    for win, rows in ((first, 2), (whole, n), (ps.KvWindow(pages, reqs, ctx, off, 4, n, w.n_pages), 4)):
+        out.fill_(3.0)
+        p.build_dev(win)
+        graph.replay()
+        torch.cuda.synchronize()
+        # (cut otherwise, so rounded otherwise: two bf16 results apart by two roundings of the weights and the results)
+        assert torch.allclose(out[:rows].float(), ref[:rows].float(), rtol=2.0 ** -7, atol=2.0 ** -7 * 6)
+        assert (out[rows:] == 3).all() and not (out[:rows] == 3).all(-1).any()
+
+
 def test_a_plan_that_was_only_captured_is_no_plan_yet(ps, sc):
     heads, kv, dim, bt = 8, 2, 64, 16
     w = Window([2], [(0, 40, 1), (0, 50, 2)], bt)
