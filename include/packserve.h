@@ -547,9 +547,9 @@ ps_status ps_kv_read_dev(ps_ctx* ctx, const ps_kv_cache* cache, const ps_kv_wind
 /*
  * A plan: how the attention of one window is cut into work, and the memory
  * for it (the context's; allocated here, so not while a stream is captured, and
- * freed by ps_attend_plan_destroy, or with the context).  It serves windows of at most max_req requests and max_rows rows
- * with n_heads query heads over n_kv_heads (a divisor of n_heads) and the
- * given head_dim and block_tokens.  ps_attend_plan_destroy waits for the
+ * freed by ps_attend_plan_destroy, or with the context).  It serves windows of
+ * at most max_req requests and max_rows rows with n_heads query heads over
+ * n_kv_heads (a divisor of n_heads) and the given head_dim and block_tokens.  ps_attend_plan_destroy waits for the
  * device's work and gives the memory back to the device, also while a stream is
  * being captured (whose work it leaves alone).  No graph that holds the plan may
  * run afterwards.

@@ -23,9 +23,10 @@
 // are staged (exact but for fp16's range), so one kernel serves both.
 //
 // Scores, maxima, sums and results are in fp32 throughout.  Two things are rounded to the
-// 16-bit type: the weights, which the second product takes in it (each by half a step at
+// 16-bit type: the weights, since the matrix cores' operands are 16 bits (in two parts they
+// would be twice the second product), each by half a step at
 // most, 2^-8 of its own size in bf16 and 2^-11 in fp16, so a result by no more than that of
-// sum p |v|; the sum that divides them takes them as they were), and the result.  fp16 has
+// sum p |v| (the sum that divides them takes them as they were); and the result.  fp16 has
 // no such half step below 2^-14, where a weight is off by 2^-25: there all weights are 2^10
 // times what they stand for (weight_lift), a row's largest is 2^10 at least, and T small
 // ones are off by T 2^-35 max|v| in the result at most.
